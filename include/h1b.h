@@ -436,8 +436,129 @@ int h1b_read_profile(h1b_ctx *ctx, double *decode_ms, int64_t *decode_launches);
 /* Kernel launches enqueued by this context so far. */
 int64_t h1b_launch_count(const h1b_ctx *ctx);
 
+/* ---- 8-bit pages: a second cache format beside the compressed one ---------
+ *
+ * (Not a step of the paper's method.) For the layers, or the recent tokens,
+ * whose keys do not survive one bit: keys and values are kept as 8-bit codes
+ * with one fp32 scale per token and KV head, and attention is the ordinary
+ * softmax(scale q k) v, causal, optionally limited to a window of last tokens
+ * and a few first ones (sinks). Aged tokens go back to fp16 with h1b_kv8_read()
+ * and from there into the compressed cache with h1b_append_kv().
+ *
+ * These calls have no context: everything they work on is in two descriptions
+ * that the caller fills in, a pool of pages (one layer's) and a ragged batch,
+ * and every pointer in them is DEVICE memory that the caller owns. All calls
+ * only enqueue kernels on `stream`: they allocate nothing, keep nothing from
+ * one call for the next, may be captured into CUDA graphs, and calls on
+ * different pools, batches and workspaces may overlap. The descriptions are
+ * HOST structures and are read before a call returns.
+ *
+ * One quantised row x of d numbers (fp16 or bf16), amax = max |x_i|:
+ *   H1B_KV8_INT8   scale = fp32(amax / 127),  code_i = x_i * 127 / amax to the
+ *                  nearest integer, ties to even
+ *   H1B_KV8_E4M3   scale = fp32(amax / 448),  code_i = x_i * 448 / amax to the
+ *                  nearest 8-bit floating-point number e4m3, ties to even
+ *   A row of zeros has scale 0 and codes 0. A row that holds an infinity or a
+ *   NaN has scale NaN and codes 0: it reads back as NaN, and makes NaN of every
+ *   query row that sees it and of no other.
+ * The number a code stands for is code * scale.
+ */
+#define H1B_KV8_INT8 0
+#define H1B_KV8_E4M3 1
+#define H1B_TYPE_F16  0
+#define H1B_TYPE_BF16 1
+
+typedef struct {             /* one layer's pages; all pointers DEVICE               */
+    void *k, *v;             /* 8-bit codes [n_pages][n_kv_heads][page_tokens][d],   */
+                             /* 16-byte aligned                                      */
+    float *k_scale, *v_scale;/* [n_pages][n_kv_heads][page_tokens], 16-byte aligned  */
+    int32_t n_pages;         /* >= 1                                                 */
+    int32_t n_kv_heads;      /* Hkv >= 1                                             */
+    int32_t page_tokens;     /* a multiple of 16                                     */
+    int32_t head_dim;        /* d: 64 or 128                                         */
+    int32_t format;          /* H1B_KV8_*                                            */
+    int32_t device;          /* CUDA device ordinal of all pointers and the stream   */
+} h1b_kv8_pool;
+
+/* A ragged batch. The tensors of a call hold n_rows rows, sequence after
+ * sequence: rows [row_start[b], row_start[b + 1]) belong to sequence b and are
+ * its last n_b = row_start[b + 1] - row_start[b] cached tokens; row r is the
+ * token at position kv_len[b] - row_start[b + 1] + r. n_b may be 0. Rows from
+ * row_start[n_seqs] on (and before row_start[0]) belong to nobody: they are not
+ * read, and outputs keep what they held there. Token t of sequence b lives in
+ * page block_table[b][t / page_tokens]; entries whose tokens no row sees are
+ * not read (pages that a window has left behind may be given away).
+ * The lengths and tables are read by the kernels, so a replayed graph works on
+ * what they hold then. They are checked there too, and never lead outside the
+ * pool: `status`, when not NULL, receives one of these codes (the caller clears
+ * it; of several, one stays) if something does not fit:
+ *   H1B_ERR_INVALID_ARG  row_start goes down or beyond n_rows, kv_len is
+ *                        negative, or a row lies before the sequence's first
+ *                        token (it is not written, reads as zeros, sees nothing)
+ *   H1B_ERR_CAPACITY     kv_len exceeds table_width * page_tokens (tokens beyond
+ *                        are not written, read as zeros, are seen by nobody)
+ *   H1B_ERR_BOUNDS       a block table entry that was needed is outside
+ *                        [0, n_pages) (its tokens likewise)
+ *   H1B_ERR_TIMEOUT      a kernel gave up a bounded wait (output undefined)
+ * Two rows of one h1b_kv8_append() must not have the same place (a page that
+ * two sequences share may be read by both and appended to by none). */
+typedef struct {
+    const int32_t *block_table; /* DEVICE [n_seqs][table_width]                      */
+    const int32_t *kv_len;      /* DEVICE [n_seqs]: cached tokens, new ones included */
+    const int32_t *row_start;   /* DEVICE [n_seqs + 1]                               */
+    int32_t *status;            /* DEVICE [1], nullable                              */
+    int32_t n_seqs;             /* >= 0                                              */
+    int32_t table_width;        /* >= 1; table_width * page_tokens <= 2^30           */
+    int32_t n_rows;             /* rows in the call's tensors, >= 0                  */
+} h1b_kv8_batch;
+
+/* Rows of heads: element (row, head, i) at data + row * row_stride + head *
+ * head_stride + i, in elements. DEVICE, 16-byte aligned, both strides multiples
+ * of 8; inputs may be slices of a larger tensor, or repeat themselves (stride
+ * 0); the rows and heads of an output must not overlap. */
+typedef struct {
+    void *data;
+    int64_t row_stride, head_stride;
+} h1b_kv8_rows;
+
+/* Quantise and append: row r of every sequence (keys k, values v, both
+ * [n_rows][Hkv][d] of type `dtype`) is written to its place in the pages. */
+int h1b_kv8_append(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8_rows *k,
+                   const h1b_kv8_rows *v, int dtype, void *stream);
+
+/* Read back: the keys and values of row r's token, code * scale rounded once to
+ * `dtype`, into row r of k and v ([n_rows][Hkv][d]; either may be NULL). */
+int h1b_kv8_read(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8_rows *k,
+                 const h1b_kv8_rows *v, int dtype, void *stream);
+
+/* Attention of the batch's rows over the cached tokens (append them first).
+ * The row at position p sees the tokens t <= p and, with window > 0, of those
+ * only t > p - window and t < sinks. Query head h reads KV head h / (Hq / Hkv).
+ *   q, out  [n_rows][Hq][d] of type `dtype`; out = softmax(scale q k) v. Sums,
+ *           maxima and products are held in fp32; the weights are rounded to
+ *           fp16 before they multiply the values.
+ *   lse     DEVICE fp32 [n_rows][Hq], nullable: the natural logarithm of the
+ *           sum of exp(scale q k) over the tokens seen (for joining the result
+ *           with attention over other tokens). A row that sees nothing gets
+ *           zeros and lse = -infinity.
+ *   scale   finite
+ *   max_rows  the largest n_b of the batch as far as the host knows it (1 for a
+ *           decode step; n_rows is always right): it chooses kernels and
+ *           launch sizes only, every row is computed whatever it says.
+ *   workspace  DEVICE, 16-byte aligned, at least h1b_kv8_attention_bytes() of
+ *           the same arguments (which may be 0: then it may be NULL). Its
+ *           contents need not be kept or cleared; two calls that may overlap on
+ *           the GPU need a workspace each. */
+size_t h1b_kv8_attention_bytes(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, int n_q_heads,
+                               int window, int sinks, int max_rows);
+int h1b_kv8_attention(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8_rows *q,
+                      const h1b_kv8_rows *out, float *lse, int n_q_heads, int dtype, float scale,
+                      int window, int sinks, int max_rows, void *workspace, size_t workspace_bytes,
+                      void *stream);
+
 /* Text of the last error recorded on this context ("" if none). With ctx ==
- * NULL: the text of the last failed h1b_init_projection() on this thread. */
+ * NULL: the text of the last failed h1b_init_projection() or h1b_kv8_ call on
+ * this thread. */
 const char *h1b_last_error(const h1b_ctx *ctx);
 
 #ifdef __cplusplus

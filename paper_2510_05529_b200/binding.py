@@ -35,6 +35,20 @@ class h1b_config(ctypes.Structure):
                                                        ("n_pages", ctypes.c_int32)]
 
 
+class h1b_kv8_pool(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + \
+               [(n, ctypes.c_int32) for n in ("n_pages", "n_kv_heads", "page_tokens", "head_dim", "format", "device")]
+
+
+class h1b_kv8_batch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("block_table", "kv_len", "row_start", "status")] + \
+               [(n, ctypes.c_int32) for n in ("n_seqs", "table_width", "n_rows")]
+
+
+class h1b_kv8_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -100,6 +114,11 @@ def load_library(rebuild: bool = True) -> ctypes.CDLL:
         "h1b_read_profile": (ctypes.c_int, [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]),
         "h1b_launch_count": (ctypes.c_int64, [vp]),
         "h1b_last_error": (ctypes.c_char_p, [vp]),
+        "h1b_kv8_append": (ctypes.c_int, [vp, vp, vp, vp, ctypes.c_int, vp]),
+        "h1b_kv8_read": (ctypes.c_int, [vp, vp, vp, vp, ctypes.c_int, vp]),
+        "h1b_kv8_attention_bytes": (ctypes.c_size_t, [vp, vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int]),
+        "h1b_kv8_attention": (ctypes.c_int, [vp, vp, vp, vp, vp, ctypes.c_int, ctypes.c_int, ctypes.c_float, ctypes.c_int,
+                                             ctypes.c_int, ctypes.c_int, vp, ctypes.c_size_t, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -426,6 +445,162 @@ class H1BCache:
 
     def h1b_launch_count(self) -> int:
         return int(self.lib.h1b_launch_count(self._h))
+
+
+_KV8_FORMATS = {torch.int8: 0, torch.float8_e4m3fn: 1}
+_KV8_TYPES = {torch.float16: 0, torch.bfloat16: 1}
+
+
+def _int32(what: str, x) -> int:
+    if not -2 ** 31 <= x < 2 ** 31:                      # (ctypes would keep the low bits)
+        raise ValueError("%s = %d is no 32-bit number" % (what, x))
+    return int(x)
+
+
+def _kv8_rows(t: torch.Tensor, what: str, heads: int, d: int, dtype, device) -> h1b_kv8_rows:
+    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype:
+        raise TypeError("%s must be a tensor of dtype %s on %s" % (what, dtype, device))
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d:
+        raise ValueError("%s must be [n_rows, %d, %d], got %s" % (what, heads, d, tuple(shape)))
+    row, head, last = t.stride()
+    if last != 1:
+        raise ValueError("the channels of %s must be contiguous" % what)
+    return h1b_kv8_rows(t.data_ptr(), row, head)
+
+
+class KV8Pages:
+    """One layer's pool of 8-bit pages over tensors of the caller's: k_pages, v_pages int8 or float8_e4m3fn
+    [n_pages, Hkv, page_tokens, d] (the dtype is the format), k_scale, v_scale fp32 [n_pages, Hkv, page_tokens], all
+    contiguous. The object keeps the tensors alive and a status word for h1b_kv8_poll_status(); it holds no lengths.
+
+    A ragged batch is three int32 CUDA tensors: block_table [B, W], kv_len [B] (cached tokens, the new ones included) and
+    row_start [B + 1]: rows row_start[b] .. row_start[b + 1] - 1 of the call's tensors are the last cached tokens of
+    sequence b. They are read by the kernels, so a captured graph may replay on other contents."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        self.lib = load_library()
+        for name, t in (("k_pages", k_pages), ("v_pages", v_pages), ("k_scale", k_scale), ("v_scale", v_scale)):
+            if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous() or t.device != k_pages.device:
+                raise TypeError("%s must be a contiguous CUDA tensor on the device of k_pages" % name)
+        if k_pages.dtype not in _KV8_FORMATS or v_pages.dtype != k_pages.dtype:
+            raise TypeError("k_pages and v_pages must be int8 or float8_e4m3fn, got %s, %s" % (k_pages.dtype, v_pages.dtype))
+        if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+            raise TypeError("k_scale and v_scale must be float32")
+        if k_pages.dim() != 4 or v_pages.shape != k_pages.shape or k_scale.shape != k_pages.shape[:3] or \
+                v_scale.shape != k_scale.shape:
+            raise ValueError("pages must be [n_pages, Hkv, page_tokens, d], scales [n_pages, Hkv, page_tokens]")
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
+        self.device = k_pages.device
+        n_pages, self.n_kv_heads, page_tokens, self.head_dim = (int(x) for x in k_pages.shape)
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._status = self.status.data_ptr()
+        self._pool = h1b_kv8_pool(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n_pages,
+                                  self.n_kv_heads, page_tokens, self.head_dim, _KV8_FORMATS[k_pages.dtype],
+                                  self.device.index)
+        self._pool_ref = ctypes.byref(self._pool)
+
+    def _check(self, rc: int):
+        if rc != H1B_OK:
+            raise H1BError(rc, (self.lib.h1b_last_error(None) or b"").decode())
+
+    def _stream(self, stream):
+        return torch.cuda.current_stream(self.device) if stream is None else stream
+
+    def _empty(self, shape, dtype, stream):
+        """A new tensor for use on `stream`: memory that another stream's pending work may still use is not handed out."""
+        if stream == torch.cuda.current_stream(self.device):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _batch(self, block_table, kv_len, row_start, n_rows: int) -> h1b_kv8_batch:
+        device, i32 = self.device, torch.int32
+        for name, t in (("block_table", block_table), ("kv_len", kv_len), ("row_start", row_start)):
+            if not isinstance(t, torch.Tensor) or t.dtype != i32 or t.device != device or not t.is_contiguous():
+                raise TypeError("%s must be a contiguous int32 tensor on %s" % (name, device))
+        shape = block_table.shape
+        if len(shape) != 2 or kv_len.shape != shape[:1] or row_start.dim() != 1 or row_start.shape[0] != shape[0] + 1:
+            raise ValueError("block_table must be [B, W], kv_len [B], row_start [B + 1]")
+        return h1b_kv8_batch(block_table.data_ptr(), kv_len.data_ptr(), row_start.data_ptr(), self._status, shape[0],
+                             shape[1], n_rows)
+
+    def h1b_kv8_append(self, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,
+                       row_start: torch.Tensor, stream=None):
+        """k, v: fp16 or bf16 CUDA [n_rows, Hkv, d] (rows and heads may be strided): quantised into their places."""
+        if k.dtype not in _KV8_TYPES:
+            raise TypeError("k must be float16 or bfloat16, got %s" % k.dtype)
+        if k.shape != v.shape:
+            raise ValueError("k and v must have the same shape")
+        kr = _kv8_rows(k, "k", self.n_kv_heads, self.head_dim, k.dtype, self.device)
+        vr = _kv8_rows(v, "v", self.n_kv_heads, self.head_dim, k.dtype, self.device)
+        batch = self._batch(block_table, kv_len, row_start, k.shape[0])
+        self._check(self.lib.h1b_kv8_append(self._pool_ref, ctypes.byref(batch), ctypes.byref(kr), ctypes.byref(vr),
+                                            _KV8_TYPES[k.dtype], self._stream(stream).cuda_stream))
+
+    def h1b_kv8_read(self, block_table: torch.Tensor, kv_len: torch.Tensor, row_start: torch.Tensor, n_rows: int | None = None,
+                     dtype=torch.float16, k: torch.Tensor | None = None, v: torch.Tensor | None = None, stream=None):
+        """Rows row_start[b] .. of every sequence read back -> (k, v) of `dtype` [n_rows, Hkv, d]. Given k and / or v, those are
+        filled (and only those); else two new tensors of n_rows rows."""
+        stream = self._stream(stream)
+        if k is None and v is None:
+            if n_rows is None:
+                raise ValueError("n_rows, k or v must be given")
+            if dtype not in _KV8_TYPES:
+                raise TypeError("dtype must be float16 or bfloat16, got %s" % dtype)
+            k, v = (self._empty((n_rows, self.n_kv_heads, self.head_dim), dtype, stream) for _ in "kv")
+        given = k if k is not None else v
+        if given.dtype not in _KV8_TYPES:
+            raise TypeError("k and v must be float16 or bfloat16, got %s" % given.dtype)
+        if k is not None and v is not None and k.shape != v.shape:
+            raise ValueError("k and v must have the same shape")
+        if n_rows is not None and n_rows != given.shape[0]:
+            raise ValueError("n_rows is %d, the tensors have %d rows" % (n_rows, given.shape[0]))
+        kr, vr = (None if t is None else
+                  ctypes.byref(_kv8_rows(t, name, self.n_kv_heads, self.head_dim, given.dtype, self.device))
+                  for t, name in ((k, "k"), (v, "v")))
+        batch = self._batch(block_table, kv_len, row_start, given.shape[0])
+        self._check(self.lib.h1b_kv8_read(self._pool_ref, ctypes.byref(batch), kr, vr, _KV8_TYPES[given.dtype],
+                                          stream.cuda_stream))
+        return k, v
+
+    def h1b_kv8_attention(self, q: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor, row_start: torch.Tensor,
+                          scale: float, window: int = 0, sinks: int = 0, max_rows: int | None = None,
+                          out: torch.Tensor | None = None, return_lse: bool = False, stream=None):
+        """q: fp16 or bf16 CUDA [n_rows, Hq, d] -> out of q's dtype and shape; with return_lse (out, lse), lse fp32 [n_rows, Hq].
+        window = 0: every token up to the row's own; else its last `window` and the sequence's first `sinks`. max_rows: the
+        largest number of rows of one sequence, if the caller knows it (1 for a decode step); it only chooses kernels."""
+        dtype, device = q.dtype, self.device
+        if dtype not in _KV8_TYPES:
+            raise TypeError("q must be float16 or bfloat16, got %s" % dtype)
+        if q.dim() != 3:
+            raise ValueError("q must be [n_rows, Hq, d]")
+        n_rows, hq, _ = q.shape
+        qr = _kv8_rows(q, "q", hq, self.head_dim, dtype, device)
+        stream = self._stream(stream)
+        window, sinks, max_rows = _int32("window", window), _int32("sinks", sinks), _int32("max_rows", n_rows if max_rows is None else max_rows)
+        if out is None:
+            out = self._empty((n_rows, hq, self.head_dim), dtype, stream)
+        elif out.shape != q.shape:
+            raise ValueError("out must have q's shape")
+        orow = _kv8_rows(out, "out", hq, self.head_dim, dtype, device)
+        batch = self._batch(block_table, kv_len, row_start, n_rows)
+        batch_ref = ctypes.byref(batch)
+        need = self.lib.h1b_kv8_attention_bytes(self._pool_ref, batch_ref, hq, window, sinks, max_rows)
+        workspace = self._empty((need,), torch.uint8, stream) if need else None
+        lse = self._empty((n_rows, hq), torch.float32, stream) if return_lse else None
+        self._check(self.lib.h1b_kv8_attention(
+            self._pool_ref, batch_ref, ctypes.byref(qr), ctypes.byref(orow), None if lse is None else lse.data_ptr(), hq,
+            _KV8_TYPES[dtype], scale, window, sinks, max_rows, None if workspace is None else workspace.data_ptr(), need,
+            stream.cuda_stream))
+        return (out, lse) if return_lse else out
+
+    def h1b_kv8_poll_status(self):
+        """Synchronises; raises H1BError if a kernel met something in a batch that does not fit (see h1b_kv8_batch), and clears it."""
+        code = int(self.status.item())
+        if code != H1B_OK:
+            self.status.zero_()
+            raise H1BError(code, "reported by a kernel of an h1b_kv8_ call")
 
 
 def unpack_words(words: np.ndarray, m: int) -> np.ndarray:

@@ -209,6 +209,21 @@ int fail(h1b_ctx *ctx, int code, const char *fmt, ...) {
     return code;
 }
 
+}  // namespace
+
+// What h1b_last_error(NULL) returns on this thread, for calls that have no context.
+int h1b::report_error(int code, const char *fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    try { g_init_error = buf; } catch (...) {}                   // (no memory for the text: the code says it)
+    return code;
+}
+
+namespace {
+
 #define H1B_CUDA(ctx, expr)                                                                   \
     do {                                                                                      \
         cudaError_t e_ = (expr);                                                              \

@@ -34,5 +34,7 @@ cudaError_t launch_set_len(int32_t *len, int n_layers, int max_batch, int seq, i
 // Scores of key words [w0, w0 + nw) of every cached token of one slab against qwords[0 .. nw).
 cudaError_t launch_debug_scores(const CacheAddr &ca, int layer, int b, int kvh, const uint32_t *qwords, int len,
                                 int w0, int nw, int32_t *score, cudaStream_t st);
+// The text behind h1b_last_error(NULL) on this thread; returns `code` (h1b_api.cu).
+int report_error(int code, const char *fmt, ...);
 
 }  // namespace h1b

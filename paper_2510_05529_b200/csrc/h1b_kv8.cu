@@ -1,0 +1,591 @@
+// 8-bit pages: quantise-and-append, read-back, and attention for few rows per sequence (decode steps, short chunks).
+#include "h1b_kv8.cuh"
+
+namespace h1b {
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------------------------
+// Append and read. One row of d numbers is handled by d / 8 lanes (8 numbers, 16 bytes, each), keys and values side by
+// side in one warp; a warp takes `heads` KV heads of one row, so the walk over the batch and the page table is done once
+// for all of them.
+// ------------------------------------------------------------------------------------------------------------------
+struct Kv8Io {
+    Kv8Params P;
+    h1b_kv8_rows k, v;
+    int heads, groups;                     // heads per warp, warps per row
+};
+
+// Where row r's token lives: its place in the pool, in tokens of one KV head ((page * hkv + head) * page_tokens + offset
+// with head = 0), or -1.
+__device__ __forceinline__ int64_t kv8_place(const Kv8Params &P, const Kv8Seq &s, int r) {
+    const int pos = s.kv - s.n + (r - s.start);
+    if (pos < 0) { kv8_report(P, H1B_ERR_INVALID_ARG); return -1; }
+    if (pos >= P.cap) { kv8_report(P, H1B_ERR_CAPACITY); return -1; }
+    const int col = pos / P.page_tokens, page = P.table[(int64_t)s.b * P.table_width + col];
+    if (page < 0 || page >= P.n_pages) { kv8_report(P, H1B_ERR_BOUNDS); return -1; }
+    return (int64_t)page * P.hkv * P.page_tokens + (pos - col * P.page_tokens);
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Io io, const int bf16) {
+    constexpr int LANES = D / 8, VECS = 32 / LANES;              // lanes per vector, vectors (key or value rows) per warp
+    constexpr float TOP = FMT == H1B_KV8_INT8 ? 127.f : 448.f;
+    const Kv8Params &P = io.P;
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    const int64_t r64 = unit / io.groups;
+    if (r64 >= P.n_rows) return;                                 // (whole warps)
+    const int r = (int)r64;
+    const int h0 = (int)(unit - r64 * io.groups) * io.heads, h1 = min(h0 + io.heads, P.hkv);
+    Kv8Seq s;
+    if (!kv8_seq_of_row(P, r, lane, &s)) return;
+    const int64_t at = kv8_place(P, s, r);
+    if (at < 0) return;
+    const int sub = lane % LANES;
+    for (int x = h0 * 2 + lane / LANES; x < (h1 * 2 + VECS - 1) / VECS * VECS; x += VECS) {   // x = head * 2 + (0 key, 1 value)
+        const int h = x >> 1;
+        const bool live = h < h1;
+        const h1b_kv8_rows &src = (x & 1) ? io.v : io.k;
+        uint4 raw = make_uint4(0, 0, 0, 0);
+        if (live)
+            raw = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(src.data) + (int64_t)r * src.row_stride +
+                                                   (int64_t)h * src.head_stride + sub * 8);
+        float f[8];
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        float amax = 0.f;
+        bool odd = false;                                        // an infinity or a NaN
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 p = pair_to_float2(w[i], bf16);
+            f[2 * i] = p.x; f[2 * i + 1] = p.y;
+            amax = fmaxf(amax, fmaxf(fabsf(p.x), fabsf(p.y)));
+            odd |= !(fabsf(p.x) <= 3.402823466e38f) || !(fabsf(p.y) <= 3.402823466e38f);
+        }
+#pragma unroll
+        for (int o = 1; o < LANES; o <<= 1) {
+            amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, o));
+            odd |= (bool)__shfl_xor_sync(~0u, (int)odd, o);
+        }
+        // TOP * x is exact in fp32 (7 + 11 bits) and the quotient correctly rounded; quotients of such numbers that are
+        // not ties lie at least 2^-16 of themselves away from one, so the codes are those of the exact quotient.
+        uint32_t lo = 0, hi = 0;
+        if (!odd && amax > 0.f) {
+            const float down = amax > 1e30f ? 0x1p-16f : 1.f, by = amax * down;   // TOP * x stays finite
+            float q[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) q[i] = __fdiv_rn(f[i] * down * TOP, by);
+            if (FMT == H1B_KV8_INT8) {
+                uint32_t c[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) c[i] = (uint32_t)__float2int_rn(q[i]) & 255u;
+                lo = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
+                hi = c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24;
+            } else {
+                uint16_t c[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c[i]) : "f"(q[2 * i + 1]), "f"(q[2 * i]));
+                lo = c[0] | (uint32_t)c[1] << 16;
+                hi = c[2] | (uint32_t)c[3] << 16;
+            }
+        }
+        if (!live) continue;
+        const int64_t row = at + (int64_t)h * P.page_tokens;
+        *reinterpret_cast<uint2 *>(((x & 1) ? P.v : P.k) + row * D + sub * 8) = make_uint2(lo, hi);
+        if (sub == 0) ((x & 1) ? P.vs : P.ks)[row] = odd ? __int_as_float(0x7FC00000) : __fdiv_rn(amax, TOP);
+    }
+}
+
+template <int D, int FMT>
+__global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Io io, const int bf16) {
+    constexpr int LANES = D / 8, VECS = 32 / LANES;
+    const Kv8Params &P = io.P;
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    const int64_t r64 = unit / io.groups;
+    if (r64 >= P.n_rows) return;
+    const int r = (int)r64;
+    const int h0 = (int)(unit - r64 * io.groups) * io.heads, h1 = min(h0 + io.heads, P.hkv);
+    Kv8Seq s;
+    if (!kv8_seq_of_row(P, r, lane, &s)) return;
+    const int64_t at = kv8_place(P, s, r);
+    const int sub = lane % LANES;
+    for (int x = h0 * 2 + lane / LANES; x < h1 * 2; x += VECS) {
+        const int h = x >> 1;
+        const h1b_kv8_rows &dst = (x & 1) ? io.v : io.k;
+        if (!dst.data) continue;
+        uint32_t w[4] = {0, 0, 0, 0};
+        if (at >= 0) {
+            const int64_t row = at + (int64_t)h * P.page_tokens;
+            const uint2 c = *reinterpret_cast<const uint2 *>(((x & 1) ? P.v : P.k) + row * D + sub * 8);
+            const float sc = ((x & 1) ? P.vs : P.ks)[row] * kv8_unit<FMT>();   // (a power of two: exact)
+            uint32_t hh[4];
+            kv8_codes4<FMT>(c.x, hh[0], hh[1]);
+            kv8_codes4<FMT>(c.y, hh[2], hh[3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 p = half2_bits_to_float2(hh[i]);
+                w[i] = float2_to_pair(p.x * sc, p.y * sc, bf16);
+            }
+        }
+        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(dst.data) + (int64_t)r * dst.row_stride +
+                                   (int64_t)h * dst.head_stride + sub * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+template <bool APPEND>
+cudaError_t launch_io(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_rows &v, int d, int fmt, int bf16,
+                      cudaStream_t st) {
+    Kv8Io io;
+    io.P = P; io.k = k; io.v = v;
+    // few rows: a warp per two vectors (latency); many: a warp takes up to eight heads
+    io.heads = 256 / d / 2;
+    while (io.heads < 8 && (int64_t)P.n_rows * ((P.hkv + io.heads - 1) / io.heads) > 148 * 64) io.heads *= 2;
+    io.groups = (P.hkv + io.heads - 1) / io.heads;
+    const int64_t warps = (int64_t)P.n_rows * io.groups;
+    const int warps_per_block = warps < 148 * 8 ? 1 : 8;
+    const unsigned grid = (unsigned)((warps + warps_per_block - 1) / warps_per_block);
+#define H1B_KV8_IO(D, F)                                                                          \
+    if (APPEND) kv8_append_kernel<D, F><<<grid, warps_per_block * 32, 0, st>>>(io, bf16);         \
+    else kv8_read_kernel<D, F><<<grid, warps_per_block * 32, 0, st>>>(io, bf16)
+    if (d == 128 && fmt == H1B_KV8_INT8) { H1B_KV8_IO(128, H1B_KV8_INT8); }
+    else if (d == 128) { H1B_KV8_IO(128, H1B_KV8_E4M3); }
+    else if (fmt == H1B_KV8_INT8) { H1B_KV8_IO(64, H1B_KV8_INT8); }
+    else { H1B_KV8_IO(64, H1B_KV8_E4M3); }
+#undef H1B_KV8_IO
+    return cudaGetLastError();
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// Attention, few rows. A block of four warps takes one tile (up to 8 * NB (row, head of the group) pairs of a sequence
+// that share a KV head) and one part of the tokens that the tile sees; the warps take its blocks of 16 tokens in turn,
+// each through a ring of its own in shared memory that 16-byte asynchronous copies fill, so nothing in the loop is
+// block-wide.
+//   S^T = K Q^T    (16 tokens x 8 NB rows)   mma m16n8k16, A = the codes as exact fp16 numbers, B = the query rows
+//   w   = 2^(S ks - m) vs / sigma            softmax weights, online; the value's scale goes into the weight
+//   O^T += V^T w   (d channels x 8 NB rows)  A = the codes again, B = the weights in fp16
+// m and sigma (a power of two) are references that follow the row's largest score and the largest value scale lazily:
+// the accumulators are only rescaled when a score exceeds m by 2 (in log2) or a scale exceeds 4 sigma, so the weights,
+// carried times 2^11, stay below 2^15 and keep fp16's full precision down to 2^-25 of the largest one. One rounding to fp16
+// (2^-12 on average) vanishes beside that of a bf16 result, but would add as much again to an fp16 result's: there (SPLIT)
+// a second product carries what the rounding left, w = hi + lo to 2^-22, at no cost in time where the loads are the bound.
+// ------------------------------------------------------------------------------------------------------------------
+constexpr int kRowsStages = 4;
+constexpr int kRowsWarps = 4;
+constexpr float kLazy = 2.f;
+constexpr float kWeightUnit = 2048.f;
+
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+
+template <int D>
+__host__ __device__ constexpr int rows_stage_bytes() { return 32 * D + 128 + 16; }
+template <int D, int NB>
+__host__ __device__ constexpr int rows_smem_bytes() {
+    const int ring = kRowsWarps * kRowsStages * rows_stage_bytes<D>(), merge = kRowsWarps * 8 * NB * (D + 2) * 4;
+    return ring > merge ? ring : merge;
+}
+
+template <int D, int FMT, int NB, bool SPLIT>
+__global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_kernel(const Kv8Params P, const Kv8Attn A) {
+    extern __shared__ __align__(128) unsigned char smem[];
+    constexpr int R = 8 * NB, STAGE = rows_stage_bytes<D>();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int gi = lane >> 2, tj = lane & 3;                     // row of A / column of B, and the pair of k, of this lane
+    const int kvh = blockIdx.y, split = blockIdx.z;
+    const uint32_t ring = smem_addr(smem) + warp * kRowsStages * STAGE;
+
+    for (int idx = blockIdx.x; idx < A.tiles; idx += gridDim.x) {
+        Kv8Seq s;
+        int tile;
+        if (!kv8_find_tile(P, A, idx, R, lane, &s, &tile)) break;
+        const int pair0 = tile * R, pairs = min(R, s.n * A.group - pair0);
+        const int tok0 = pair0 / A.group, tok1 = (pair0 + pairs - 1) / A.group;
+        const int pos0 = s.kv - s.n + tok0, pos1 = s.kv - s.n + tok1;
+        if (pos0 < 0 && split == 0) kv8_report(P, H1B_ERR_INVALID_ARG);
+        const Kv8Span span = kv8_span(P, A, pos0, pos1);
+        // the tile's blocks in parts of `per`, a multiple of four (one per warp) and at least two per warp
+        const int per = max((((span.count + A.splits - 1) / A.splits) + 3) & ~3, 2 * kRowsWarps);
+        const int parts = max(1, (span.count + per - 1) / per);
+        if (split >= parts) continue;
+        const int j0 = split * per, j1 = min(j0 + per, span.count);
+        const int n_mine = j1 - j0 > warp ? (j1 - j0 - warp + kRowsWarps - 1) / kRowsWarps : 0;
+
+        // ---- the copies: block i of this warp into stage i % kRowsStages; page numbers come 32 blocks at a time ----
+        const int32_t *table = P.table + (int64_t)s.b * P.table_width;
+        int page_lane = -1;
+        auto issue = [&](int i) {
+            if (i < n_mine) {
+                if ((i & 31) == 0) {
+                    const int j = j0 + warp + (i + lane) * kRowsWarps;
+                    page_lane = i + lane < n_mine ? table[span.token(j) / P.page_tokens] : -1;
+                    if (i + lane < n_mine && (page_lane < 0 || page_lane >= P.n_pages)) {
+                        kv8_report(P, H1B_ERR_BOUNDS);
+                        page_lane = -1;
+                    }
+                }
+                const int page = __shfl_sync(~0u, page_lane, i & 31);
+                const int t = span.token(j0 + warp + i * kRowsWarps);
+                const uint32_t st = ring + (i % kRowsStages) * STAGE;
+                if (page >= 0) {
+                    const int64_t at = ((int64_t)page * P.hkv + kvh) * P.page_tokens + t % P.page_tokens;
+                    const uint8_t *kp = P.k + at * D, *vp = P.v + at * D;
+#pragma unroll
+                    for (int c = 0; c < D / 32; ++c) {
+                        const int x = lane + 32 * c, r = x / (D / 16), ch = x % (D / 16);
+                        const uint32_t kd = D == 128 ? r * 128 + ((ch ^ ((r & 1) << 2)) << 4) : x << 4;
+                        const uint32_t vd = D == 128 ? r * 128 + ((ch ^ (r & 7)) << 4)
+                                                     : (r >> 1) * 128 + (((((r & 1) << 2) | ch) ^ (((r >> 1) & 3) << 1)) << 4);
+                        cp_async_16(st + kd, kp + x * 16, 16);
+                        cp_async_16(st + 16 * D + vd, vp + x * 16, 16);
+                    }
+                    if (lane < 8)
+                        cp_async_16(st + 32 * D + lane * 16, (lane < 4 ? P.ks : P.vs) + at + (lane & 3) * 4, 16);
+                }
+                if (lane == 0)                                   // the block's first token, or -1: nobody sees it
+                    *reinterpret_cast<int *>(smem + (st - smem_addr(smem)) + 32 * D + 128) = page >= 0 ? t : -1;
+            }
+            cp_async_commit();
+        };
+#pragma unroll
+        for (int i = 0; i < kRowsStages - 1; ++i) issue(i);
+
+        // ---- the query rows, as B operands: lane (n = gi, k pair tj) holds channels 16 (tj + 4 c) .. + 15 of row gi ----
+        uint32_t qf[NB][D / 16][2];
+        float qs[NB][2];                                         // what turns a dot product of codes into a score, rows 2 tj, + 1
+        int pos[NB][2];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int x = nb * 8 + gi, tok = (pair0 + x) / A.group, head = kvh * A.group + (pair0 + x) % A.group;
+            const bool live = x < pairs;
+            const uint16_t *qp = static_cast<const uint16_t *>(A.q) + (int64_t)(s.start + tok) * A.q_rs + (int64_t)head * A.q_hs;
+            float2 f[D / 16][2];
+            float amax = 0.f;
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+                uint4 u[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+                if (live) {
+                    u[0] = *reinterpret_cast<const uint4 *>(qp + 16 * (tj + 4 * c));
+                    u[1] = *reinterpret_cast<const uint4 *>(qp + 16 * (tj + 4 * c) + 8);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 &uu = u[i >> 1];
+                    f[c * 4 + i][0] = pair_to_float2((i & 1) ? uu.z : uu.x, A.bf16);
+                    f[c * 4 + i][1] = pair_to_float2((i & 1) ? uu.w : uu.y, A.bf16);
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        amax = fmaxf(amax, fmaxf(fabsf(f[c * 4 + i][y].x), fabsf(f[c * 4 + i][y].y)));
+                }
+            }
+            amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
+            amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
+            const int e = kv8_row_exponent(amax);
+            const float up = pow2i(-e);
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) qf[nb][i][y] = pack_f16x2(f[i][y].x * up, f[i][y].y * up);
+            const float unit = A.scale_log2 * kv8_unit<FMT>() * pow2i(e);
+            const int t0 = s.kv - s.n + tok;
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                qs[nb][y] = __shfl_sync(~0u, unit, (2 * tj + y) * 4);
+                pos[nb][y] = __shfl_sync(~0u, t0, (2 * tj + y) * 4);
+            }
+        }
+
+        float o[NB][D / 16][4], m[NB][2], l[NB][2];
+        float sigma = 0.f, wscale = 0.f;                         // wscale = kWeightUnit / sigma
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) o[nb][i][0] = o[nb][i][1] = o[nb][i][2] = o[nb][i][3] = 0.f;
+            m[nb][0] = m[nb][1] = -INFINITY;
+            l[nb][0] = l[nb][1] = 0.f;
+        }
+
+        for (int i = 0; i < n_mine; ++i) {
+            cp_async_wait_group<kRowsStages - 2>();
+            __syncwarp();                                        // every lane's copies of block i are there; block i - 1 is read
+            issue(i + kRowsStages - 1);
+            const unsigned char *st = smem + warp * kRowsStages * STAGE + (i % kRowsStages) * STAGE;
+            const int t = *reinterpret_cast<const int *>(st + 32 * D + 128);
+            if (t < 0) continue;
+            // ---- scores ----
+            float c[NB][4];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) c[nb][0] = c[nb][1] = c[nb][2] = c[nb][3] = 0.f;
+#pragma unroll
+            for (int h = 0; h < D / 64; ++h) {
+                const int ch = D == 128 ? (tj + 4 * h) ^ ((gi & 1) << 2) : tj;
+                const uint4 ka = *reinterpret_cast<const uint4 *>(st + gi * D + ch * 16);
+                const uint4 kb = *reinterpret_cast<const uint4 *>(st + (gi + 8) * D + ch * 16);
+                const uint32_t wa[4] = {ka.x, ka.y, ka.z, ka.w}, wb[4] = {kb.x, kb.y, kb.z, kb.w};
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    uint32_t a0, a1, a2, a3;
+                    kv8_codes4<FMT>(wa[x], a0, a2);
+                    kv8_codes4<FMT>(wb[x], a1, a3);
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb)
+                        mma_f16_16816(c[nb], a0, a1, a2, a3, qf[nb][h * 4 + x][0], qf[nb][h * 4 + x][1]);
+                }
+            }
+            const float *sc = reinterpret_cast<const float *>(st + 32 * D);
+            const float ks0 = sc[gi], ks1 = sc[gi + 8];
+            float vs0 = sc[16 + gi], vs1 = sc[16 + gi + 8];
+            const int t0 = t + gi, t1 = t0 + 8;
+            // all rows of the tile see all 16 tokens, or each pair is looked at
+            const bool whole = t + 15 <= pos0 && (!A.window || t > pos1 - A.window || t + 15 < A.sinks);
+            bool see[NB][4];
+            float big = 0.f;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int tt = (y & 2) ? t1 : t0, p = pos[nb][y & 1];
+                    see[nb][y] = whole || (tt <= p && (!A.window || tt > p - A.window || tt < A.sinks));
+                    c[nb][y] = see[nb][y] ? c[nb][y] * ((y & 2) ? ks1 : ks0) * qs[nb][y & 1] : -INFINITY;
+                    big = fmaxf(big, c[nb][y] - m[nb][y & 1] > kLazy ? 1.f : 0.f);
+                }
+            if (!whole) {                                        // scales of tokens that no row sees say nothing
+                if (!(t0 <= span.hi && (t0 >= span.lo || t0 < span.sinks))) vs0 = 0.f;
+                if (!(t1 <= span.hi && (t1 >= span.lo || t1 < span.sinks))) vs1 = 0.f;
+            }
+            const float vbig = fmaxf(vs0 <= 3.402823466e38f ? vs0 : 0.f, vs1 <= 3.402823466e38f ? vs1 : 0.f);
+            if (__any_sync(~0u, big > 0.f || vbig > 4.f * sigma)) {
+                float mx = vbig;
+#pragma unroll
+                for (int x = 1; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, x));
+                float turn = 1.f;                                // old sigma / new sigma
+                if (mx > 4.f * sigma) {
+                    const int e = clampi((int)(__float_as_uint(mx) >> 23) - 126, -120, 126);   // 2^e > mx
+                    const float next = pow2i(e);
+                    turn = sigma / next;
+                    sigma = next;
+                    wscale = kWeightUnit * pow2i(-e);
+                }
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        float top = fmaxf(c[nb][y], c[nb][y + 2]);
+                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
+                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
+                        top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
+                        const float next = fmaxf(m[nb][y], top);
+                        const float f = next > m[nb][y] ? ex2_approx(m[nb][y] - next) : 1.f;   // (from -inf: 0)
+                        m[nb][y] = next;
+                        l[nb][y] *= f;
+#pragma unroll
+                        for (int x = 0; x < D / 16; ++x) { o[nb][x][y] *= f * turn; o[nb][x][y + 2] *= f * turn; }
+                    }
+            }
+            // ---- weights: fp16, rounded once; a token that a row does not see gets weight zero whatever its scale holds ----
+            const float g0 = vs0 * wscale, g1 = vs1 * wscale;
+            uint32_t b[NB][2], b_lo[NB][2];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                float p[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) p[y] = see[nb][y] ? ex2_approx(c[nb][y] - m[nb][y & 1]) : 0.f;
+                l[nb][0] += p[0] + p[2];
+                l[nb][1] += p[1] + p[3];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) p[y] = see[nb][y] ? p[y] * ((y & 2) ? g1 : g0) : 0.f;
+#pragma unroll
+                for (int y = 0; y < 2; ++y) {
+                    const uint32_t hi = pack_f16x2(p[2 * y], p[2 * y + 1]);
+                    b[nb][y] = movmatrix_trans(hi);
+                    if (SPLIT) {
+                        const float2 back = half2_bits_to_float2(hi);
+                        b_lo[nb][y] = movmatrix_trans(pack_f16x2(p[2 * y] - back.x, p[2 * y + 1] - back.y));
+                    }
+                }
+            }
+            // ---- values: lane (m = gi, k pair tj) holds channels (D / 8) gi .. of tokens 2 tj, 2 tj + 1, + 8, + 9 ----
+            const unsigned char *vst = st + 16 * D;
+            uint32_t w[4][D / 32];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                const int r = 2 * tj + (y & 1) + (y & 2) * 4;
+                if (D == 128) {
+                    const uint4 u = *reinterpret_cast<const uint4 *>(vst + r * 128 + ((gi ^ (r & 7)) << 4));
+                    w[y][0] = u.x; w[y][1] = u.y; w[y][D / 32 - 2] = u.z; w[y][D / 32 - 1] = u.w;
+                } else {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(
+                        vst + (r >> 1) * 128 + (((((r & 1) << 2) | (gi >> 1)) ^ (((r >> 1) & 3) << 1)) << 4) + (gi & 1) * 8);
+                    w[y][0] = u.x; w[y][1] = u.y;
+                }
+            }
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x) {
+                uint32_t lo[4], hi[4];
+                kv8_codes4x2<FMT>(w[0][x], w[1][x], lo);
+                kv8_codes4x2<FMT>(w[2][x], w[3][x], hi);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    mma_f16_16816(o[nb][2 * x], lo[0], lo[1], hi[0], hi[1], b[nb][0], b[nb][1]);
+                    mma_f16_16816(o[nb][2 * x + 1], lo[2], lo[3], hi[2], hi[3], b[nb][0], b[nb][1]);
+                    if (SPLIT) {
+                        mma_f16_16816(o[nb][2 * x], lo[0], lo[1], hi[0], hi[1], b_lo[nb][0], b_lo[nb][1]);
+                        mma_f16_16816(o[nb][2 * x + 1], lo[2], lo[3], hi[2], hi[3], b_lo[nb][0], b_lo[nb][1]);
+                    }
+                }
+            }
+        }
+        cp_async_wait_group<0>();
+
+        // ---- the four warps' results meet in shared memory: [warp][row][d], then m and l [warp][row] ----
+        __syncthreads();
+        float *acc = reinterpret_cast<float *>(smem), *ml = acc + kRowsWarps * R * D;
+        const float unit = sigma * (kv8_unit<FMT>() / kWeightUnit);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                const int row = nb * 8 + 2 * tj + y;
+                float sum = l[nb][y];
+                sum += __shfl_xor_sync(~0u, sum, 4);
+                sum += __shfl_xor_sync(~0u, sum, 8);
+                sum += __shfl_xor_sync(~0u, sum, 16);
+                float *a = acc + (warp * R + row) * D + gi * (D / 8);
+#pragma unroll
+                for (int x = 0; x < D / 16; ++x) {
+                    a[2 * x] = o[nb][x][y] * unit;
+                    a[2 * x + 1] = o[nb][x][y + 2] * unit;
+                }
+                // (a row whose every score is NaN has no maximum, and is not an empty row)
+                if (gi == 0) { ml[(warp * R + row) * 2] = sum != sum ? sum : m[nb][y]; ml[(warp * R + row) * 2 + 1] = sum; }
+            }
+        __syncthreads();
+        constexpr int PER = D / 2;                               // channel pairs of a row
+        for (int x = threadIdx.x; x < pairs * PER; x += kRowsWarps * 32) {
+            const int row = x / PER, ch = (x % PER) * 2;
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kRowsWarps; ++w) {
+                const float mw = ml[(w * R + row) * 2];
+                top = (mw > top || mw != mw) ? mw : top;
+            }
+            float sum = 0.f, a0 = 0.f, a1 = 0.f;
+#pragma unroll
+            for (int w = 0; w < kRowsWarps; ++w) {
+                const float mw = ml[(w * R + row) * 2], f = mw == -INFINITY ? 0.f : ex2_approx(mw - top);
+                sum += f * ml[(w * R + row) * 2 + 1];
+                a0 += f * acc[(w * R + row) * D + ch];
+                a1 += f * acc[(w * R + row) * D + ch + 1];
+            }
+            const bool empty = top == -INFINITY;
+            if (empty) { a0 = a1 = 0.f; } else { a0 /= sum; a1 /= sum; }
+            const int tok = (pair0 + row) / A.group, head = kvh * A.group + (pair0 + row) % A.group;
+            const int64_t line = (int64_t)(s.start + tok) * A.hq + head;
+            const float lse2 = empty ? -INFINITY : top + log2f(sum);
+            if (parts == 1) {
+                *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(A.out) + (int64_t)(s.start + tok) * A.o_rs +
+                                              (int64_t)head * A.o_hs + ch) = float2_to_pair(a0, a1, A.bf16);
+                if (A.lse && ch == 0) A.lse[line] = lse2 * kLn2;
+            } else {
+                *reinterpret_cast<float2 *>(A.part_acc + (line * A.splits + split) * D + ch) = make_float2(a0, a1);
+                if (ch == 0) A.part_lse[line * A.splits + split] = lse2;
+            }
+        }
+        __syncthreads();                                         // the ring is free for the next tile's copies
+    }
+}
+
+// Joins the parts of the rows whose tokens were dealt into more than one: out = sum_s 2^(lse_s - lse) out_s. A warp per
+// (row, head).
+template <int D>
+__global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Params P, const Kv8Attn A, const int R, const int unit_blocks,
+                                                       const int min_blocks) {
+    const int lane = threadIdx.x & 31;
+    const int64_t line = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
+    const int r = (int)(line / A.hq), head = (int)(line - (int64_t)r * A.hq);
+    if (r >= P.n_rows) return;
+    Kv8Seq s;
+    if (!kv8_seq_of_row(P, r, lane, &s)) return;
+    const int all = s.n * A.group;
+    if (all < A.min_pairs || all > A.max_pairs) return;
+    // the same split of the same tile as the attention kernel's
+    const int pair0 = ((r - s.start) * A.group + head % A.group) / R * R, pairs = min(R, all - pair0);
+    const Kv8Span span = kv8_span(P, A, s.kv - s.n + pair0 / A.group, s.kv - s.n + (pair0 + pairs - 1) / A.group);
+    const int per = max(((span.count + A.splits - 1) / A.splits + unit_blocks - 1) / unit_blocks * unit_blocks, min_blocks);
+    const int parts = max(1, (span.count + per - 1) / per);
+    if (parts == 1) return;
+    const float *pl = A.part_lse + line * A.splits, *pa = A.part_acc + line * A.splits * D;
+    float top = -INFINITY;
+    bool nan = false;
+    for (int i = lane; i < parts; i += 32) { top = fmaxf(top, pl[i]); nan |= pl[i] != pl[i]; }
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    nan = __any_sync(~0u, nan);
+    float sum = 0.f, a[D / 32];
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x) a[x] = 0.f;
+    for (int i = 0; i < parts; ++i) {
+        const float f = pl[i] == -INFINITY ? 0.f : ex2_approx(pl[i] - top);
+        sum += f;
+        if (f == 0.f) continue;
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) {
+            const float2 v = *reinterpret_cast<const float2 *>(pa + (int64_t)i * D + x * 64 + lane * 2);
+            a[2 * x] += f * v.x;
+            a[2 * x + 1] += f * v.y;
+        }
+    }
+    const bool empty = top == -INFINITY && !nan;
+    uint16_t *op = static_cast<uint16_t *>(A.out) + (int64_t)r * A.o_rs + (int64_t)head * A.o_hs;
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x)
+        *reinterpret_cast<uint32_t *>(op + x * 64 + lane * 2) =
+            empty ? 0u : float2_to_pair(a[2 * x] / sum, a[2 * x + 1] / sum, A.bf16);
+    if (A.lse && lane == 0) A.lse[line] = empty ? -INFINITY : (top + log2f(sum)) * kLn2;
+}
+
+template <int D, int FMT, int NB, bool SPLIT>
+cudaError_t launch_rows_of(const Kv8Params &P, const Kv8Attn &A, int grid_tiles, cudaStream_t st) {
+    constexpr int bytes = rows_smem_bytes<D, NB>();
+    const cudaError_t e = cudaFuncSetAttribute(kv8_rows_kernel<D, FMT, NB, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    const dim3 grid((unsigned)grid_tiles, (unsigned)P.hkv, (unsigned)A.splits);
+    kv8_rows_kernel<D, FMT, NB, SPLIT><<<grid, kRowsWarps * 32, bytes, st>>>(P, A);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_kv8_append(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_rows &v, int d, int fmt, int bf16,
+                              cudaStream_t st) {
+    return launch_io<true>(P, k, v, d, fmt, bf16, st);
+}
+cudaError_t launch_kv8_read(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_rows &v, int d, int fmt, int bf16,
+                            cudaStream_t st) {
+    return launch_io<false>(P, k, v, d, fmt, bf16, st);
+}
+
+cudaError_t launch_kv8_rows(const Kv8Params &P, const Kv8Attn &A, int d, int fmt, int rows_per_tile, int grid_tiles,
+                            cudaStream_t st) {
+    cudaError_t e;
+#define H1B_KV8_ROWS(D, F)                                                                                        \
+    e = rows_per_tile == 8 ? (A.bf16 ? launch_rows_of<D, F, 1, false> : launch_rows_of<D, F, 1, true>)(P, A, grid_tiles, st) \
+                           : (A.bf16 ? launch_rows_of<D, F, 2, false> : launch_rows_of<D, F, 2, true>)(P, A, grid_tiles, st)
+    if (d == 128 && fmt == H1B_KV8_INT8) { H1B_KV8_ROWS(128, H1B_KV8_INT8); }
+    else if (d == 128) { H1B_KV8_ROWS(128, H1B_KV8_E4M3); }
+    else if (fmt == H1B_KV8_INT8) { H1B_KV8_ROWS(64, H1B_KV8_INT8); }
+    else { H1B_KV8_ROWS(64, H1B_KV8_E4M3); }
+#undef H1B_KV8_ROWS
+    if (e != cudaSuccess || A.splits == 1) return e;
+    const int64_t lines = (int64_t)P.n_rows * A.hq;
+    const unsigned grid = (unsigned)((lines + 3) / 4);
+    if (d == 128) kv8_join_kernel<128><<<grid, 128, 0, st>>>(P, A, rows_per_tile, kRowsWarps, 2 * kRowsWarps);
+    else kv8_join_kernel<64><<<grid, 128, 0, st>>>(P, A, rows_per_tile, kRowsWarps, 2 * kRowsWarps);
+    return cudaGetLastError();
+}
+
+}  // namespace h1b

@@ -1,0 +1,213 @@
+// Host side of the 8-bit pages (h1b_kv8_*): checks of the arguments, launch shapes, launches.
+#include <algorithm>
+#include <cmath>
+
+#include <cuda_runtime.h>
+
+#include "h1b_kv8.cuh"
+
+using namespace h1b;
+
+namespace {
+
+// The device of the pool for the length of a call; the caller's current device afterwards.
+struct DeviceScope {
+    int before = -1;
+    cudaError_t err;
+    explicit DeviceScope(int device) {
+        err = cudaGetDevice(&before);
+        if (err == cudaSuccess && before != device) err = cudaSetDevice(device);
+        else if (err == cudaSuccess) before = -1;
+    }
+    ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
+};
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int check_pool(const h1b_kv8_pool *p) {
+    if (!p) return report_error(H1B_ERR_NULL, "pool is NULL");
+    if (p->head_dim != 64 && p->head_dim != 128)
+        return report_error(H1B_ERR_UNSUPPORTED, "head_dim = %d: 64 or 128", p->head_dim);
+    if (p->format != H1B_KV8_INT8 && p->format != H1B_KV8_E4M3)
+        return report_error(H1B_ERR_INVALID_ARG, "unknown format %d", p->format);
+    if (p->n_pages < 1 || p->n_kv_heads < 1 || p->n_kv_heads > 1024 || p->device < 0)
+        return report_error(H1B_ERR_INVALID_ARG, "n_pages = %d, n_kv_heads = %d, device = %d out of range", p->n_pages,
+                            p->n_kv_heads, p->device);
+    if (p->page_tokens < kKv8Block || p->page_tokens % kKv8Block)
+        return report_error(H1B_ERR_INVALID_ARG, "page_tokens = %d: a multiple of %d", p->page_tokens, kKv8Block);
+    if (!p->k || !p->v || !p->k_scale || !p->v_scale) return report_error(H1B_ERR_NULL, "a pool pointer is NULL");
+    if (!aligned16(p->k) || !aligned16(p->v) || !aligned16(p->k_scale) || !aligned16(p->v_scale))
+        return report_error(H1B_ERR_INVALID_ARG, "a pool pointer is not 16-byte aligned");
+    return H1B_OK;
+}
+
+int check_batch(const h1b_kv8_pool *p, const h1b_kv8_batch *b) {
+    if (!b) return report_error(H1B_ERR_NULL, "batch is NULL");
+    if (b->n_seqs < 0 || b->n_rows < 0 || b->table_width < 1)
+        return report_error(H1B_ERR_INVALID_ARG, "n_seqs = %d, n_rows = %d, table_width = %d out of range", b->n_seqs,
+                            b->n_rows, b->table_width);
+    if ((int64_t)b->table_width * p->page_tokens > (1 << 30))
+        return report_error(H1B_ERR_INVALID_ARG, "table_width * page_tokens = %lld exceeds 2^30",
+                            (long long)b->table_width * p->page_tokens);
+    if (b->n_seqs > 0 && (!b->block_table || !b->kv_len || !b->row_start))
+        return report_error(H1B_ERR_NULL, "block_table, kv_len or row_start is NULL");
+    return H1B_OK;
+}
+
+int check_rows(const char *name, const h1b_kv8_rows *t, int64_t rows, int heads, int d, bool output, bool nullable) {
+    if (!t) return nullable ? H1B_OK : report_error(H1B_ERR_NULL, "%s is NULL", name);
+    if (rows == 0) return H1B_OK;                                // nothing is read or written
+    if (!t->data) return nullable ? H1B_OK : report_error(H1B_ERR_NULL, "%s.data is NULL", name);
+    if (!aligned16(t->data)) return report_error(H1B_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
+    if ((rows > 1 && t->row_stride % 8) || (heads > 1 && t->head_stride % 8))
+        return report_error(H1B_ERR_INVALID_ARG, "strides of %s (%lld, %lld) are not multiples of 8", name,
+                            (long long)t->row_stride, (long long)t->head_stride);
+    if (output) {
+        const int64_t rs = std::llabs(t->row_stride), hs = std::llabs(t->head_stride);
+        const bool heads_inside = (heads == 1 || hs >= d) && (rows == 1 || rs >= (heads == 1 ? d : hs * (heads - 1) + d));
+        const bool rows_inside = (rows == 1 || rs >= d) && (heads == 1 || hs >= (rows == 1 ? d : rs * (rows - 1) + d));
+        if (!heads_inside && !rows_inside)
+            return report_error(H1B_ERR_INVALID_ARG, "rows or heads of %s overlap (strides %lld, %lld)", name,
+                                (long long)t->row_stride, (long long)t->head_stride);
+    }
+    return H1B_OK;
+}
+
+int check_type(int dtype) {
+    if (dtype != H1B_TYPE_F16 && dtype != H1B_TYPE_BF16) return report_error(H1B_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+    return H1B_OK;
+}
+
+Kv8Params params_of(const h1b_kv8_pool *p, const h1b_kv8_batch *b) {
+    Kv8Params P;
+    P.k = static_cast<uint8_t *>(p->k); P.v = static_cast<uint8_t *>(p->v);
+    P.ks = p->k_scale; P.vs = p->v_scale;
+    P.table = b->block_table; P.kv_len = b->kv_len; P.row_start = b->row_start; P.status = b->status;
+    P.n_pages = p->n_pages; P.hkv = p->n_kv_heads; P.page_tokens = p->page_tokens;
+    P.n_seqs = b->n_seqs; P.table_width = b->table_width; P.n_rows = b->n_rows;
+    P.cap = b->table_width * p->page_tokens;
+    return P;
+}
+
+#define H1B_KV8_TRY(expr)                                                                                        \
+    do {                                                                                                         \
+        const cudaError_t e_ = (expr);                                                                           \
+        if (e_ != cudaSuccess) return report_error(H1B_ERR_CUDA, "%s: %s", #expr, cudaGetErrorString(e_));       \
+    } while (0)
+
+int check_io(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8_rows *k, const h1b_kv8_rows *v, int dtype,
+             bool output) {
+    int rc = check_pool(pool);
+    if (rc == H1B_OK) rc = check_batch(pool, batch);
+    if (rc == H1B_OK) rc = check_rows("k", k, batch->n_rows, pool->n_kv_heads, pool->head_dim, output, output);
+    if (rc == H1B_OK) rc = check_rows("v", v, batch->n_rows, pool->n_kv_heads, pool->head_dim, output, output);
+    if (rc == H1B_OK) rc = check_type(dtype);
+    return rc;
+}
+
+// How the attention of a batch is launched; a function of sizes only.
+struct AttnPlan {
+    int rows_per_tile, tiles, grid_tiles, splits;
+    size_t bytes;
+};
+
+AttnPlan plan_of(const h1b_kv8_pool *p, const h1b_kv8_batch *b, int hq, int window, int sinks, int max_rows) {
+    AttnPlan a;
+    const int64_t group = hq / p->n_kv_heads, pairs = (int64_t)b->n_rows * group;
+    const int64_t most = std::min<int64_t>(std::max(max_rows, 1), b->n_rows) * group;
+    a.rows_per_tile = most <= 8 ? 8 : 16;
+    a.tiles = (int)(pairs / a.rows_per_tile + std::min(b->n_seqs, b->n_rows));
+    a.grid_tiles = (int)std::min<int64_t>(a.tiles, (int64_t)b->n_seqs * ((most + a.rows_per_tile - 1) / a.rows_per_tile));
+    // Parts: enough blocks for four waves of the GPU's 148 SMs at three or more blocks an SM, so that ragged lengths even
+    // out; no more than the tokens that a row can see give work to (two blocks of 16 tokens a warp, four warps).
+    const int64_t cap = (int64_t)b->table_width * p->page_tokens;
+    const int64_t seen = window ? std::min<int64_t>(cap, (int64_t)window + sinks + max_rows + 32) : cap;
+    const int64_t blocks = (int64_t)a.grid_tiles * p->n_kv_heads;
+    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>((148 * 12 + blocks - 1) / blocks, (seen + 127) / 128));
+    a.splits = std::min(a.splits, 256);
+    a.bytes = a.splits > 1 ? (size_t)b->n_rows * hq * a.splits * (p->head_dim + 1) * sizeof(float) : 0;
+    return a;
+}
+
+int check_attention(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, int hq, int window, int sinks, int max_rows) {
+    int rc = check_pool(pool);
+    if (rc == H1B_OK) rc = check_batch(pool, batch);
+    if (rc != H1B_OK) return rc;
+    if (hq < 1 || hq % pool->n_kv_heads || hq / pool->n_kv_heads > 128)
+        return report_error(H1B_ERR_INVALID_ARG, "%d query heads over %d KV heads: a multiple, at most 128 times", hq,
+                            pool->n_kv_heads);
+    if ((int64_t)batch->n_rows * hq > (1 << 30))
+        return report_error(H1B_ERR_INVALID_ARG, "n_rows * n_q_heads exceeds 2^30");
+    if (window < 0 || sinks < 0 || window > (1 << 30) || sinks > (1 << 30) || max_rows < 0)
+        return report_error(H1B_ERR_INVALID_ARG, "window = %d, sinks = %d, max_rows = %d out of range", window, sinks, max_rows);
+    return H1B_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int h1b_kv8_append(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8_rows *k, const h1b_kv8_rows *v,
+                   int dtype, void *stream) {
+    const int rc = check_io(pool, batch, k, v, dtype, false);
+    if (rc != H1B_OK) return rc;
+    if (batch->n_rows == 0 || batch->n_seqs == 0) return H1B_OK;
+    DeviceScope dev(pool->device);
+    H1B_KV8_TRY(dev.err);
+    H1B_KV8_TRY(launch_kv8_append(params_of(pool, batch), *k, *v, pool->head_dim, pool->format, dtype,
+                                  static_cast<cudaStream_t>(stream)));
+    return H1B_OK;
+}
+
+int h1b_kv8_read(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8_rows *k, const h1b_kv8_rows *v,
+                 int dtype, void *stream) {
+    const int rc = check_io(pool, batch, k, v, dtype, true);
+    if (rc != H1B_OK) return rc;
+    const h1b_kv8_rows none{nullptr, 0, 0};
+    const h1b_kv8_rows &kk = k ? *k : none, &vv = v ? *v : none;
+    if (batch->n_rows == 0 || batch->n_seqs == 0 || (!kk.data && !vv.data)) return H1B_OK;
+    DeviceScope dev(pool->device);
+    H1B_KV8_TRY(dev.err);
+    H1B_KV8_TRY(launch_kv8_read(params_of(pool, batch), kk, vv, pool->head_dim, pool->format, dtype,
+                                static_cast<cudaStream_t>(stream)));
+    return H1B_OK;
+}
+
+size_t h1b_kv8_attention_bytes(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, int n_q_heads, int window, int sinks,
+                               int max_rows) {
+    if (check_attention(pool, batch, n_q_heads, window, sinks, max_rows) != H1B_OK) return 0;
+    if (batch->n_rows == 0 || batch->n_seqs == 0) return 0;
+    return plan_of(pool, batch, n_q_heads, window, sinks, max_rows).bytes;
+}
+
+int h1b_kv8_attention(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8_rows *q, const h1b_kv8_rows *out,
+                      float *lse, int n_q_heads, int dtype, float scale, int window, int sinks, int max_rows,
+                      void *workspace, size_t workspace_bytes, void *stream) {
+    int rc = check_attention(pool, batch, n_q_heads, window, sinks, max_rows);
+    if (rc == H1B_OK) rc = check_rows("q", q, batch->n_rows, n_q_heads, pool->head_dim, false, false);
+    if (rc == H1B_OK) rc = check_rows("out", out, batch->n_rows, n_q_heads, pool->head_dim, true, false);
+    if (rc == H1B_OK) rc = check_type(dtype);
+    if (rc != H1B_OK) return rc;
+    if (!std::isfinite(scale)) return report_error(H1B_ERR_INVALID_ARG, "scale is not finite");
+    if (batch->n_rows == 0 || batch->n_seqs == 0) return H1B_OK;
+    const AttnPlan plan = plan_of(pool, batch, n_q_heads, window, sinks, max_rows);
+    if (plan.bytes && (!workspace || workspace_bytes < plan.bytes || !aligned16(workspace)))
+        return report_error(H1B_ERR_WORKSPACE, "workspace needs %zu bytes, 16-byte aligned (got %zu at %p)", plan.bytes,
+                            workspace ? workspace_bytes : (size_t)0, workspace);
+    DeviceScope dev(pool->device);
+    H1B_KV8_TRY(dev.err);
+    Kv8Attn A;
+    A.q = q->data; A.out = out->data; A.lse = lse;
+    A.q_rs = q->row_stride; A.q_hs = q->head_stride; A.o_rs = out->row_stride; A.o_hs = out->head_stride;
+    A.hq = n_q_heads; A.group = n_q_heads / pool->n_kv_heads; A.bf16 = dtype == H1B_TYPE_BF16;
+    A.scale_log2 = (float)((double)scale * 1.4426950408889634074);
+    A.window = window; A.sinks = window ? sinks : 0;
+    A.splits = plan.splits; A.tiles = plan.tiles; A.min_pairs = 1; A.max_pairs = 1 << 30; A.reserved = 0;
+    A.part_acc = static_cast<float *>(workspace);
+    A.part_lse = A.part_acc ? A.part_acc + (size_t)batch->n_rows * n_q_heads * plan.splits * pool->head_dim : nullptr;
+    H1B_KV8_TRY(launch_kv8_rows(params_of(pool, batch), A, pool->head_dim, pool->format, plan.rows_per_tile, plan.grid_tiles,
+                                static_cast<cudaStream_t>(stream)));
+    return H1B_OK;
+}
+
+}  // extern "C"
