@@ -484,68 +484,70 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_ker
             const bool empty = top == -INFINITY;
             if (empty) { a0 = a1 = 0.f; } else { a0 /= sum; a1 /= sum; }
             const int tok = (pair0 + row) / A.group, head = kvh * A.group + (pair0 + row) % A.group;
-            const int64_t line = (int64_t)(s.start + tok) * A.hq + head;
+            const int64_t part = (((int64_t)idx * P.hkv + kvh) * R + row) * A.splits + split;
             const float lse2 = empty ? -INFINITY : top + log2f(sum);
             if (parts == 1) {
                 *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(A.out) + (int64_t)(s.start + tok) * A.o_rs +
                                               (int64_t)head * A.o_hs + ch) = float2_to_pair(a0, a1, A.bf16);
-                if (A.lse && ch == 0) A.lse[line] = lse2 * kLn2;
+                if (A.lse && ch == 0) A.lse[(int64_t)(s.start + tok) * A.hq + head] = lse2 * kLn2;
             } else {
-                *reinterpret_cast<float2 *>(A.part_acc + (line * A.splits + split) * D + ch) = make_float2(a0, a1);
-                if (ch == 0) A.part_lse[line * A.splits + split] = lse2;
+                *reinterpret_cast<float2 *>(A.part_acc + part * D + ch) = make_float2(a0, a1);
+                if (ch == 0) A.part_lse[part] = lse2;
             }
         }
         __syncthreads();                                         // the ring is free for the next tile's copies
     }
 }
 
-// Joins the parts of the rows whose tokens were dealt into more than one: out = sum_s 2^(lse_s - lse) out_s. A warp per
-// (row, head).
+// Joins the parts of the rows whose tokens were dealt into more than one: out = sum_s 2^(lse_s - lse) out_s. A block takes
+// eight pairs of a tile, a warp two of them.
 template <int D>
 __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Params P, const Kv8Attn A, const int R, const int unit_blocks,
                                                        const int min_blocks) {
-    const int lane = threadIdx.x & 31;
-    const int64_t line = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int r = (int)(line / A.hq), head = (int)(line - (int64_t)r * A.hq);
-    if (r >= P.n_rows) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int idx = blockIdx.x / P.hkv, kvh = blockIdx.x % P.hkv;
     Kv8Seq s;
-    if (!kv8_seq_of_row(P, r, lane, &s)) return;
-    const int all = s.n * A.group;
-    if (all < A.min_pairs || all > A.max_pairs) return;
+    int tile;
+    if (!kv8_find_tile(P, A, idx, R, lane, &s, &tile)) return;
     // the same split of the same tile as the attention kernel's
-    const int pair0 = ((r - s.start) * A.group + head % A.group) / R * R, pairs = min(R, all - pair0);
+    const int pair0 = tile * R, pairs = min(R, s.n * A.group - pair0);
     const Kv8Span span = kv8_span(P, A, s.kv - s.n + pair0 / A.group, s.kv - s.n + (pair0 + pairs - 1) / A.group);
     const int per = max(((span.count + A.splits - 1) / A.splits + unit_blocks - 1) / unit_blocks * unit_blocks, min_blocks);
     const int parts = max(1, (span.count + per - 1) / per);
     if (parts == 1) return;
-    const float *pl = A.part_lse + line * A.splits, *pa = A.part_acc + line * A.splits * D;
-    float top = -INFINITY;
-    bool nan = false;
-    for (int i = lane; i < parts; i += 32) { top = fmaxf(top, pl[i]); nan |= pl[i] != pl[i]; }
+    for (int row = blockIdx.y * 8 + warp; row < min(pairs, (int)blockIdx.y * 8 + 8); row += 4) {
+        const int64_t part = (((int64_t)idx * P.hkv + kvh) * R + row) * A.splits;
+        const float *pl = A.part_lse + part, *pa = A.part_acc + part * D;
+        float top = -INFINITY;
+        bool nan = false;
+        for (int i = lane; i < parts; i += 32) { top = fmaxf(top, pl[i]); nan |= pl[i] != pl[i]; }
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-    nan = __any_sync(~0u, nan);
-    float sum = 0.f, a[D / 32];
+        for (int o = 1; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+        nan = __any_sync(~0u, nan);
+        float sum = 0.f, a[D / 32];
 #pragma unroll
-    for (int x = 0; x < D / 32; ++x) a[x] = 0.f;
-    for (int i = 0; i < parts; ++i) {
-        const float f = pl[i] == -INFINITY ? 0.f : ex2_approx(pl[i] - top);
-        sum += f;
-        if (f == 0.f) continue;
+        for (int x = 0; x < D / 32; ++x) a[x] = 0.f;
+#pragma unroll 4
+        for (int i = 0; i < parts; ++i) {
+            const float f = pl[i] == -INFINITY ? 0.f : ex2_approx(pl[i] - top);
+            sum += f;
 #pragma unroll
-        for (int x = 0; x < D / 64; ++x) {
-            const float2 v = *reinterpret_cast<const float2 *>(pa + (int64_t)i * D + x * 64 + lane * 2);
-            a[2 * x] += f * v.x;
-            a[2 * x + 1] += f * v.y;
+            for (int x = 0; x < D / 64; ++x) {
+                const float2 v = *reinterpret_cast<const float2 *>(pa + (int64_t)i * D + x * 64 + lane * 2);
+                a[2 * x] += f * v.x;
+                a[2 * x + 1] += f * v.y;
+            }
         }
-    }
-    const bool empty = top == -INFINITY && !nan;
-    uint16_t *op = static_cast<uint16_t *>(A.out) + (int64_t)r * A.o_rs + (int64_t)head * A.o_hs;
+        const bool empty = top == -INFINITY && !nan;
+        const int tok = (pair0 + row) / A.group, head = kvh * A.group + (pair0 + row) % A.group;
+        uint16_t *op = static_cast<uint16_t *>(A.out) + (int64_t)(s.start + tok) * A.o_rs + (int64_t)head * A.o_hs;
 #pragma unroll
-    for (int x = 0; x < D / 64; ++x)
-        *reinterpret_cast<uint32_t *>(op + x * 64 + lane * 2) =
-            empty ? 0u : float2_to_pair(a[2 * x] / sum, a[2 * x + 1] / sum, A.bf16);
-    if (A.lse && lane == 0) A.lse[line] = empty ? -INFINITY : (top + log2f(sum)) * kLn2;
+        for (int x = 0; x < D / 64; ++x)
+            *reinterpret_cast<uint32_t *>(op + x * 64 + lane * 2) =
+                empty ? 0u : float2_to_pair(a[2 * x] / sum, a[2 * x + 1] / sum, A.bf16);
+        if (A.lse && lane == 0)
+            A.lse[(int64_t)(s.start + tok) * A.hq + head] = empty ? -INFINITY : (top + log2f(sum)) * kLn2;
+    }
 }
 
 template <int D, int FMT, int NB, bool SPLIT>
@@ -581,10 +583,14 @@ cudaError_t launch_kv8_rows(const Kv8Params &P, const Kv8Attn &A, int d, int fmt
     else { H1B_KV8_ROWS(64, H1B_KV8_E4M3); }
 #undef H1B_KV8_ROWS
     if (e != cudaSuccess || A.splits == 1) return e;
-    const int64_t lines = (int64_t)P.n_rows * A.hq;
-    const unsigned grid = (unsigned)((lines + 3) / 4);
-    if (d == 128) kv8_join_kernel<128><<<grid, 128, 0, st>>>(P, A, rows_per_tile, kRowsWarps, 2 * kRowsWarps);
-    else kv8_join_kernel<64><<<grid, 128, 0, st>>>(P, A, rows_per_tile, kRowsWarps, 2 * kRowsWarps);
+    return launch_kv8_join(P, A, d, rows_per_tile, kRowsWarps, 2 * kRowsWarps, st);
+}
+
+cudaError_t launch_kv8_join(const Kv8Params &P, const Kv8Attn &A, int d, int rows_per_tile, int unit_blocks, int min_blocks,
+                            cudaStream_t st) {
+    const dim3 grid((unsigned)A.tiles * (unsigned)P.hkv, (unsigned)(rows_per_tile / 8));
+    if (d == 128) kv8_join_kernel<128><<<grid, 128, 0, st>>>(P, A, rows_per_tile, unit_blocks, min_blocks);
+    else kv8_join_kernel<64><<<grid, 128, 0, st>>>(P, A, rows_per_tile, unit_blocks, min_blocks);
     return cudaGetLastError();
 }
 

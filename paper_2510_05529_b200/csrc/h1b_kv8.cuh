@@ -36,8 +36,7 @@ struct Kv8Attn {
     int tiles;                             // no batch of n_rows rows has more tiles than this
     int min_pairs;                         // sequences with fewer (row, head of the group) pairs are another kernel's ...
     int max_pairs;                         // ... and those with more
-    int reserved;
-    float *part_acc, *part_lse;            // [n_rows * hq][splits][d], [n_rows * hq][splits] (log2)
+    float *part_acc, *part_lse;            // [tiles][hkv][pairs of a tile][splits] times [d], and alone (log2)
 };
 
 __device__ __forceinline__ void kv8_report(const Kv8Params &P, int code) {
@@ -197,6 +196,10 @@ cudaError_t launch_kv8_append(const Kv8Params &P, const h1b_kv8_rows &k, const h
 cudaError_t launch_kv8_read(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_rows &v, int d, int fmt, int bf16,
                             cudaStream_t st);
 cudaError_t launch_kv8_rows(const Kv8Params &P, const Kv8Attn &A, int d, int fmt, int rows_per_tile, int grid_tiles,
+                            cudaStream_t st);
+
+cudaError_t launch_kv8_tiles(const Kv8Params &P, const Kv8Attn &A, int d, int fmt, cudaStream_t st);
+cudaError_t launch_kv8_join(const Kv8Params &P, const Kv8Attn &A, int d, int rows_per_tile, int unit_blocks, int min_blocks,
                             cudaStream_t st);
 
 int report_error(int code, const char *fmt, ...);      // h1b_api.cu: the text behind h1b_last_error(NULL)

@@ -105,27 +105,60 @@ int check_io(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8
     return rc;
 }
 
-// How the attention of a batch is launched; a function of sizes only.
+// How the attention of a batch is launched; a function of sizes only. Sequences with at most kFewPairs (row, head of the
+// group) pairs go to the kernel for few rows, the others to the tensor-core tiles; both are launched only when the host
+// cannot tell that one of them has nothing to do.
+constexpr int kFewPairs = 32;
+
+struct AttnPart {
+    bool used = false;
+    int rows_per_tile = 0, tiles = 0, grid_tiles = 0, splits = 1, min_pairs = 1, max_pairs = 1 << 30;
+    size_t lines = 0;                                            // partial results
+};
 struct AttnPlan {
-    int rows_per_tile, tiles, grid_tiles, splits;
-    size_t bytes;
+    AttnPart few, many;
+    size_t bytes = 0;
 };
 
 AttnPlan plan_of(const h1b_kv8_pool *p, const h1b_kv8_batch *b, int hq, int window, int sinks, int max_rows) {
     AttnPlan a;
     const int64_t group = hq / p->n_kv_heads, pairs = (int64_t)b->n_rows * group;
-    const int64_t most = std::min<int64_t>(std::max(max_rows, 1), b->n_rows) * group;
-    a.rows_per_tile = most <= 8 ? 8 : 16;
-    a.tiles = (int)(pairs / a.rows_per_tile + std::min(b->n_seqs, b->n_rows));
-    a.grid_tiles = (int)std::min<int64_t>(a.tiles, (int64_t)b->n_seqs * ((most + a.rows_per_tile - 1) / a.rows_per_tile));
-    // Parts: enough blocks for four waves of the GPU's 148 SMs at three or more blocks an SM, so that ragged lengths even
-    // out; no more than the tokens that a row can see give work to (two blocks of 16 tokens a warp, four warps).
+    const int64_t rows = std::min<int64_t>(std::max(max_rows, 1), b->n_rows), most = rows * group;
+    const int64_t seqs = std::min(b->n_seqs, b->n_rows);
+    a.many.used = most > kFewPairs;
+    a.few.used = !a.many.used || (b->n_seqs > 1 && rows * b->n_seqs > b->n_rows);
     const int64_t cap = (int64_t)b->table_width * p->page_tokens;
-    const int64_t seen = window ? std::min<int64_t>(cap, (int64_t)window + sinks + max_rows + 32) : cap;
-    const int64_t blocks = (int64_t)a.grid_tiles * p->n_kv_heads;
-    a.splits = (int)std::max<int64_t>(1, std::min<int64_t>((148 * 12 + blocks - 1) / blocks, (seen + 127) / 128));
-    a.splits = std::min(a.splits, 256);
-    a.bytes = a.splits > 1 ? (size_t)b->n_rows * hq * a.splits * (p->head_dim + 1) * sizeof(float) : 0;
+    const int64_t seen = window ? std::min<int64_t>(cap, (int64_t)window + sinks + rows + 32) : cap;
+    if (a.few.used) {
+        AttnPart &f = a.few;
+        if (a.many.used) f.max_pairs = kFewPairs;
+        const int64_t here = std::min<int64_t>(most, f.max_pairs);
+        f.rows_per_tile = here <= 8 ? 8 : 16;
+        const int64_t hinted = (int64_t)b->n_seqs * ((here + f.rows_per_tile - 1) / f.rows_per_tile);
+        f.tiles = (int)(pairs / f.rows_per_tile + seqs);
+        if (a.many.used) f.tiles = (int)std::min<int64_t>(f.tiles, hinted);    // (no sequence has more)
+        f.grid_tiles = (int)std::min<int64_t>(f.tiles, hinted);
+        // Parts: enough blocks for four waves of the GPU's 148 SMs at three blocks an SM, so that ragged lengths even out;
+        // no more than the tokens that a row can see give work to (two blocks of 16 tokens a warp, four warps).
+        const int64_t blocks = (int64_t)f.grid_tiles * p->n_kv_heads;
+        // (The last limit bounds the workspace when max_rows says far less than the batch holds.)
+        f.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(148 * 12 + blocks - 1) / blocks, (seen + 127) / 128, 256,
+                                                                148 * 48 / ((int64_t)f.tiles * p->n_kv_heads)}));
+    }
+    if (a.many.used) {
+        AttnPart &m = a.many;
+        if (a.few.used) m.min_pairs = kFewPairs + 1;
+        m.rows_per_tile = 256;
+        m.tiles = m.grid_tiles = (int)(pairs / 256 + seqs);
+        // Parts only where there are too few tiles for the SMs, and of at least 512 tokens
+        const int64_t blocks = (int64_t)m.tiles * p->n_kv_heads;
+        m.splits = blocks >= 148 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(296 / blocks, seen / 512));
+    }
+    for (AttnPart *part : {&a.few, &a.many})
+        if (part->used && part->splits > 1) {
+            part->lines = (size_t)part->tiles * p->n_kv_heads * part->rows_per_tile * part->splits;
+            a.bytes += part->lines * (p->head_dim + 1) * sizeof(float);
+        }
     return a;
 }
 
@@ -202,11 +235,23 @@ int h1b_kv8_attention(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, cons
     A.hq = n_q_heads; A.group = n_q_heads / pool->n_kv_heads; A.bf16 = dtype == H1B_TYPE_BF16;
     A.scale_log2 = (float)((double)scale * 1.4426950408889634074);
     A.window = window; A.sinks = window ? sinks : 0;
-    A.splits = plan.splits; A.tiles = plan.tiles; A.min_pairs = 1; A.max_pairs = 1 << 30; A.reserved = 0;
-    A.part_acc = static_cast<float *>(workspace);
-    A.part_lse = A.part_acc ? A.part_acc + (size_t)batch->n_rows * n_q_heads * plan.splits * pool->head_dim : nullptr;
-    H1B_KV8_TRY(launch_kv8_rows(params_of(pool, batch), A, pool->head_dim, pool->format, plan.rows_per_tile, plan.grid_tiles,
-                                static_cast<cudaStream_t>(stream)));
+    const Kv8Params P = params_of(pool, batch);
+    float *at = static_cast<float *>(workspace);
+    auto take = [&](const AttnPart &part) {                      // this part's share of the workspace
+        A.splits = part.splits; A.tiles = part.tiles; A.min_pairs = part.min_pairs; A.max_pairs = part.max_pairs;
+        A.part_acc = part.lines ? at : nullptr;
+        A.part_lse = part.lines ? at + part.lines * pool->head_dim : nullptr;
+        if (part.lines) at += part.lines * (pool->head_dim + 1);
+    };
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (plan.many.used) {
+        take(plan.many);
+        H1B_KV8_TRY(launch_kv8_tiles(P, A, pool->head_dim, pool->format, st));
+    }
+    if (plan.few.used) {
+        take(plan.few);
+        H1B_KV8_TRY(launch_kv8_rows(P, A, pool->head_dim, pool->format, plan.few.rows_per_tile, plan.few.grid_tiles, st));
+    }
     return H1B_OK;
 }
 
