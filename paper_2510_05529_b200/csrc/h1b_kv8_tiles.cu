@@ -1,43 +1,63 @@
 // 8-bit pages: attention for many rows per sequence (prompts and chunks of them) on the 5th-generation tensor cores.
 //
-// One block of 13 warps takes 256 (row, head of the group) pairs of a sequence that share a KV head, as two tiles of 128
-// pairs, and one part of the tokens they see, 128 tokens at a time (eight blocks of 16, whichever blocks the span lists:
-// sinks and window need not be neighbours). The roles hand each other operands through mbarriers; nothing in the loop is
+// One block of 18 warps takes 256 (row, head of the group) pairs of a sequence that share a KV head, as two tiles of 128
+// pairs, and one part of the tokens they see, 64 tokens at a time (four blocks of 16, whichever blocks the span lists: sinks
+// and window need not be neighbours). The roles hand each other operands through mbarriers; nothing in the loop is
 // block-wide:
-//   warps 8-11   convert: codes come from the pages in 16-byte loads, one tile ahead in registers, become exact fp16
-//                numbers ONCE for all 256 pairs and go to shared memory as the matrix operands of keys and values (two
-//                of each, 128-byte swizzle; keys K-major, values with the channels contiguous, so nothing is transposed);
-//   warp 12      issues every contraction: S = Q K^T into tensor memory, O += P V with P read from tensor memory;
-//   warps 0-3    softmax of tile A, warps 4-7 of tile B, one pair (row of S) per thread: scores S * ks * qs, the row's
-//                reference, weights w = 2^(score - m) * vs / sigma in fp16, written over the scores they came from.
-// While one tile's softmax runs the tensor cores work for the other tile. m and sigma follow lazily (as in the kernel for
-// few rows): O is rescaled only when a score exceeds m by 4 (in log2) or a value scale exceeds 4 sigma; weights are
-// carried times 2^9. For fp16 results (SPLIT) a second contraction adds what rounding the weights left over.
+//   warps 8-15   convert (four warps the keys, four the values): codes come from the pages in 16-byte loads, one step
+//                ahead in registers, become exact fp16 numbers ONCE for all 256 pairs and go to shared memory as matrix
+//                operands (four of each, 128-byte swizzle; keys K-major, values with the channels contiguous, so nothing
+//                is transposed);
+//   warps 16, 17 issue the contractions of tile A and of tile B: S = Q K^T into tensor memory, O += P V with P read from
+//                tensor memory;
+//   warps 0-3    softmax of tile A, warps 4-7 of tile B, 32 rows a warp: scores S * ks * qs, the rows' references,
+//                weights w = 2^(score - m) * vs / sigma in fp16, written over the scores they came from.
+// Tensor memory holds two sets of scores for each tile, so the scores of the next step are there when a softmax warp has
+// finished with this one: with one set of 128 columns a step took softmax and contractions one after the other (7400
+// cycles for 128 tokens instead of the longer of the two). m and sigma follow lazily (as in the kernel for few rows): O is
+// rescaled only when a score exceeds m by 4 (in log2) or a value scale exceeds 4 sigma; weights are carried times 2^9. For
+// fp16 results (SPLIT) a second contraction adds what rounding the weights left over.
 // Every wait is bounded; a role that gives up records the time-out and leaves, and the block releases its tensor memory.
+#include <type_traits>
+
 #include "h1b_kv8.cuh"
 
 namespace h1b {
 
 namespace {
 
-constexpr int kTlRows = 128, kTlKeys = 128;
-constexpr int kTlThreads = 13 * 32;
-constexpr unsigned long long kTlWaitNs = 2000000000ull;
+constexpr int kTlRows = 128, kTlKeys = 64, kTlBlocks = kTlKeys / kKv8Block;
+constexpr int kTlThreads = 20 * 32;                            // warps 0-7 softmax, 8-15 convert, 16-17 issue; 18, 19 only
+                                                                // hand over their registers
+constexpr int kTlRegsLaunch = 96, kTlRegsSoftmax = 144, kTlRegsConvert = 64, kTlRegsIssue = 64;
+static_assert(256 * kTlRegsSoftmax + 256 * kTlRegsConvert + 128 * kTlRegsIssue <= kTlThreads * kTlRegsLaunch,
+              "more registers than a block is launched with");
 constexpr float kTlLazy = 4.f, kTlWeightUnit = 512.f;
 constexpr int kTlHidden = 1 << 30;                             // "first token" of a block that nobody sees: beyond every position
-constexpr int kTlScaleStages = 4;
+constexpr int kTlUnit = kTlBlocks, kTlMinBlocks = 16;         // a part is whole steps, and 256 tokens at least
+constexpr int kTlStages = 4, kTlScaleStages = 8;
+
+// What a block works on, in shared memory: each role reads what it needs where it needs it. (Kept in registers across the
+// roles' branches it was spilled, and a reload from local memory, whose lines the codes push out of the small L1, held up
+// the issuing thread for longer than its contractions took.)
+struct TlWork {
+    int64_t part0;                                               // index of (first row, this part) among the partial results
+    int go, seq, start, seq_pos, pair0, pairs, parts, lo, hi, sinks, sink_blocks, first, j0, j1, n_tiles, n_q;
+    uint32_t tmem;
+};
 
 template <int D>
 struct TlSmem {
     static constexpr int kQ1 = kTlRows * D * 2, kKV1 = kTlKeys * D * 2;
-    static constexpr int kQ = 0, kK = 2 * kQ1, kV = kK + 2 * kKV1, kScales = kV + 2 * kKV1;
-    // per scale stage: ks [128], vs' [128], blocks' first tokens [8], {first token if all 128 are in a row, else -1; turn}
-    static constexpr int kStage = 1024 + 64;
-    static constexpr int kBars = kScales + kTlScaleStages * kStage;
-    static constexpr int kTotal = kBars + 256 + 1024;            // + slack to align the operands to 1024 bytes
+    static constexpr int kQ = 0, kK = 2 * kQ1, kV = kK + kTlStages * kKV1, kScales = kV + kTlStages * kKV1;
+    // per scale stage: ks [64], vs / sigma [64], blocks' first tokens [4], {first token if all 64 are in a row, else -1; turn; sigma}
+    static constexpr int kVs = kTlKeys * 4, kFirst = 2 * kTlKeys * 4, kStage = kFirst + 32;
+    static constexpr int kRows = kScales + kTlScaleStages * kStage;              // qs [256], positions [256]
+    static constexpr int kBars = kRows + 2 * kTlRows * 8;
+    static constexpr int kTotal = kBars + 512 + 1024;            // + slack to align the operands to 1024 bytes
 };
-enum { kBarQ = 0, kBarKFull = 1, kBarKFree = 3, kBarVFull = 5, kBarVFree = 7, kBarScales = 9, kBarS = 13, kBarP = 15, kBarO = 17,
-       kBarCount = 18 };
+enum { kBarQ = 0, kBarKFull = 1, kBarKFree = 5, kBarVFull = 9, kBarVFree = 13, kBarScales = 17, kBarS = 25, kBarP = 29, kBarPV = 33,
+       kBarO = 37, kBarCount = 39 };
 
 __device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
     uint64_t r;
@@ -66,29 +86,76 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
     return r;
 }
 
-// An operand with the channels contiguous (MN-major): rows of 128 bytes (64 channels) per token, 128-byte swizzle, eight
-// tokens 1024 bytes apart, the next 64 channels 16384 bytes on.
-__device__ __forceinline__ uint64_t umma_desc_mn_sw128(uint32_t addr) {
-    uint64_t d = 0;
-    d |= (uint64_t)((addr >> 4) & 0x3FFFu);
-    d |= (uint64_t)(16384 >> 4) << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
-__device__ __forceinline__ void tmem_st_16cols_issue(uint32_t taddr, const uint32_t (&r)[16]) {
+// Matrix descriptors of operands in shared memory, 128-byte swizzle: the lower word is the start address (16-byte units) and
+// the leading offset, the upper word the stride between groups of eight rows (1024 bytes), the version and the layout. Only
+// the address changes from one contraction to the next, so the one issuing thread, which has some 50 cycles for each, adds
+// to a lower word and does nothing else.
+//   K-major: rows of 128 bytes (64 numbers along K), the leading offset is unused.
+//   MN-major (channels contiguous): rows of 128 bytes (64 channels) per token; the next 64 channels `lead` bytes on.
+constexpr uint32_t kDescHi = (1024u >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t desc_lo(uint32_t addr, uint32_t lead) { return (addr >> 4) | (lead >> 4) << 16; }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t idesc, bool add) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
-        : "memory");
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
+        ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(idesc), "r"((uint32_t)add), "n"(kDescHi) : "memory");
 }
-__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) {
-    return __all_sync(~0u, mbar_wait_bounded(bar, parity, kTlWaitNs));
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b_lo, uint32_t idesc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}"
+        ::"r"(d), "r"(a_tmem), "r"(b_lo), "r"(idesc), "r"((uint32_t)add), "n"(kDescHi) : "memory");
 }
+// Tensor memory in the layout of a matrix fragment: 16 lanes (rows) x 32 columns; register 4 b + 2 y + x of lane l holds row
+// 8 y + l / 4, column 8 b + 2 (l % 4) + x. A lane then meets 8 of 32 columns instead of all, so what belongs to a column (its
+// token's scales) is read from shared memory a quarter as often as with one row per lane: with that, the reads took most
+// of the time that shared memory has beside the contractions' operands.
+__device__ __forceinline__ void tmem_ld_frag_issue(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_tie16(uint32_t (&r)[16]) {
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
+// The store of the same fragment.
+__device__ __forceinline__ void tmem_st_frag_f32(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// 16 rows x 4 N columns of 32 bits: register 2 b + y of lane l is row 8 y + l / 4, column 4 b + l % 4.
+__device__ __forceinline__ void tmem_st_frag16(uint32_t taddr, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_frag32(uint32_t taddr, const uint32_t (&r)[8], const uint32_t (&s)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(s[0]), "r"(s[1]), "r"(s[2]), "r"(s[3]), "r"(s[4]), "r"(s[5]), "r"(s[6]), "r"(s[7]) : "memory");
+}
+// A bounded wait: a look, then at most 2^20 looks that may each park the warp for about 2 us while the phase is incomplete
+// (a second or two). It is written out at each place it is used, so it is short: the loops of the three roles have to stay
+// in the instruction cache together (when they did not, instruction fetches bound the kernel).
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity) {
+    if (mbar_try_wait(bar, parity)) return true;
+#pragma unroll 1
+    for (int i = 0; i < 1 << 20; ++i)
+        if (mbar_try_wait_parked(bar, parity, H1B_WAIT_PARK_NS)) return true;
+    return false;
+}
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(~0u, wait_phase(bar, parity)); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
-// Where the weights of contraction step ks (16 tokens) lie within the tile's 128 columns: 32 columns of scores become 16
+// Where the weights of contraction step ks (16 tokens) lie within a set of scores' 64 columns: 32 columns of scores become 16
 // columns of weights (two to a column) and 16 of their remainders.
 __device__ __forceinline__ uint32_t weight_column(int ks) { return (ks >> 1) * 32 + (ks & 1) * 8; }
 
@@ -96,53 +163,80 @@ template <int D, int FMT, bool SPLIT>
 __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Params P, const Kv8Attn A) {
     using M = TlSmem<D>;
     extern __shared__ unsigned char smem_raw[];
-    __shared__ uint32_t tmem_base_s;
+    __shared__ TlWork work_s;
+    const volatile TlWork &W = work_s;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     unsigned char *smem = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const uint32_t sm = smem_addr(smem), bars = sm + M::kBars;
     auto bar = [&](int i) { return bars + 8u * i; };
 
-    // the last tiles of a prompt see the most tokens: they go first
-    const int idx = A.tiles - 1 - (int)(blockIdx.x / P.hkv), kvh = blockIdx.x % P.hkv, split = blockIdx.z;
-    Kv8Seq s;
-    int tile;
-    if (!kv8_find_tile(P, A, idx, 2 * kTlRows, lane, &s, &tile)) return;
-    const int pair0 = tile * 2 * kTlRows, pairs = min(2 * kTlRows, s.n * A.group - pair0);
-    const int seq_pos = s.kv - s.n;                              // position of the sequence's first row
-    const int pos0 = seq_pos + pair0 / A.group, pos1 = seq_pos + (pair0 + pairs - 1) / A.group;
-    if (pos0 < 0 && split == 0) kv8_report(P, H1B_ERR_INVALID_ARG);
-    const Kv8Span span = kv8_span(P, A, pos0, pos1);
-    const int per = max(((span.count + A.splits - 1) / A.splits + 7) & ~7, 16);
-    const int parts = max(1, (span.count + per - 1) / per);
-    if (split >= parts) return;
-    const int j0 = split * per, j1 = min(j0 + per, span.count);
-    const int n_tiles = (j1 - j0 + 7) / 8, n_q = pairs > kTlRows ? 2 : 1;
-
-    if (warp == 12) tmem_alloc(smem_addr(&tmem_base_s), 512);
+    if (warp == 0) {
+        // the last tiles of a prompt see the most tokens: they go first
+        const int idx = A.tiles - 1 - (int)(blockIdx.x / P.hkv), split = blockIdx.z;
+        Kv8Seq s;
+        int tile;
+        bool go = kv8_find_tile(P, A, idx, 2 * kTlRows, lane, &s, &tile);
+        if (go) {
+            const int pair0 = tile * 2 * kTlRows, pairs = min(2 * kTlRows, s.n * A.group - pair0);
+            const int seq_pos = s.kv - s.n;                      // position of the sequence's first row
+            const int pos0 = seq_pos + pair0 / A.group, pos1 = seq_pos + (pair0 + pairs - 1) / A.group;
+            if (pos0 < 0 && split == 0) kv8_report(P, H1B_ERR_INVALID_ARG);
+            const Kv8Span span = kv8_span(P, A, pos0, pos1);
+            const int per = max(((span.count + A.splits - 1) / A.splits + kTlUnit - 1) / kTlUnit * kTlUnit, kTlMinBlocks);
+            const int parts = max(1, (span.count + per - 1) / per);
+            go = split < parts;
+            if (lane == 0) {
+                const int j0 = split * per, j1 = min(j0 + per, span.count);
+                work_s.part0 = (((int64_t)idx * P.hkv + (int)(blockIdx.x % P.hkv)) * 2 * kTlRows) * A.splits + split;
+                work_s.seq = s.b; work_s.start = s.start; work_s.seq_pos = seq_pos;
+                work_s.pair0 = pair0; work_s.pairs = pairs; work_s.parts = parts;
+                work_s.lo = span.lo; work_s.hi = span.hi; work_s.sinks = span.sinks;
+                work_s.sink_blocks = span.sink_blocks; work_s.first = span.first;
+                work_s.j0 = j0; work_s.j1 = j1;
+                work_s.n_tiles = (j1 - j0 + kTlBlocks - 1) / kTlBlocks;
+                work_s.n_q = pairs > kTlRows ? 2 : 1;
+            }
+        }
+        if (lane == 0) work_s.go = go;
+    }
+    __syncthreads();
+    if (!W.go) return;
+    if (warp == 16) tmem_alloc(smem_addr(&work_s.tmem), 512);
     if (tid == 0) {
-        const int counts[kBarCount] = {8, 4, 4, 1, 1, 4, 4, 1, 1, 4, 4, 4, 4, 1, 1, 4, 4, 1};
-#pragma unroll
-        for (int i = 0; i < kBarCount; ++i) mbar_init(bar(i), counts[i]);
+        for (int i = 0; i < kBarCount; ++i) {                    // arrivals: one a warp, or one commit
+            int n = 1;
+            if (i == kBarQ) n = 8;
+            else if (i >= kBarScales && i < kBarS) n = 8;
+            else if (i >= kBarP && i < kBarPV) n = 4;
+            else if ((i >= kBarKFull && i < kBarKFree) || (i >= kBarVFull && i < kBarVFree)) n = 4;
+            else if ((i >= kBarKFree && i < kBarVFull) || (i >= kBarVFree && i < kBarScales)) n = W.n_q;
+            mbar_init(bar(i), n);
+        }
         mbar_fence_init();
     }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = tmem_base_s;
     bool failed = false;
 
     if (warp < 8) {
+        more_registers<kTlRegsSoftmax>();
         // ---------------------------------------------------------------------------------------- softmax
-        const int qt = warp >> 2, row = tid & 127, pair = pair0 + qt * kTlRows + row;
-        const bool live = qt * kTlRows + row < pairs;
-        const int tok = pair / A.group, head = kvh * A.group + pair % A.group, pos = seq_pos + tok;
-        float qs;
-        {   // the query row: fp16 multiplied by 2^-e, negated if the scale is negative, into the K-major operand
-            const uint16_t *qp = static_cast<const uint16_t *>(A.q) + (int64_t)(s.start + tok) * A.q_rs + (int64_t)head * A.q_hs;
-            uint32_t w[D / 2];
+        // A warp has 32 rows of a tile in fragment layout: rows gi + 8 q (q = 0 .. 3) of them are this lane's, four lanes to a
+        // row. (A warp reaches the quarter of tensor memory of its number % 4.)
+        const int qt = warp >> 2, gi = lane >> 2, tj = lane & 3, row0 = (warp & 3) * 32;
+        // the query rows, two threads to a row: fp16 multiplied by 2^-e, negated if the scale is negative, into the K-major
+        // operand
+#pragma unroll 1
+        for (int r = tid >> 1; r < 2 * kTlRows; r += 128) {
+            const int half = tid & 1;
+            const int pair = W.pair0 + r, tok = pair / A.group, head = (int)(blockIdx.x % P.hkv) * A.group + pair % A.group;
+            const bool live = r < W.pairs;
+            const uint16_t *qp = static_cast<const uint16_t *>(A.q) + (int64_t)(W.start + tok) * A.q_rs + (int64_t)head * A.q_hs + half * (D / 2);
+            uint32_t w[D / 4];
             float amax = 0.f;
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
+            for (int c = 0; c < D / 16; ++c) {
                 uint4 u = make_uint4(0, 0, 0, 0);
                 if (live) u = *reinterpret_cast<const uint4 *>(qp + c * 8);
                 w[4 * c] = u.x; w[4 * c + 1] = u.y; w[4 * c + 2] = u.z; w[4 * c + 3] = u.w;
@@ -152,353 +246,437 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                     amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
                 }
             }
+            amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
             const int e = kv8_row_exponent(amax);
             const float up = A.scale_log2 < 0.f ? -pow2i(-e) : pow2i(-e);
-            unsigned char *dst = smem + M::kQ + qt * M::kQ1;
+            unsigned char *dst = smem + M::kQ + (r >> 7) * M::kQ1 + (r & 127) * 128;
 #pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
+            for (int c = 0; c < D / 16; ++c) {
                 uint32_t h[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float2 f = pair_to_float2(w[4 * c + i], A.bf16);
                     h[i] = pack_f16x2(f.x * up, f.y * up);
                 }
-                *reinterpret_cast<uint4 *>(dst + (c >> 3) * (kTlRows * 128) + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
+                const int ch = half * (D / 16) + c;
+                *reinterpret_cast<uint4 *>(dst + (ch >> 3) * (kTlRows * 128) + (((ch & 7) ^ (r & 7)) << 4)) =
                     make_uint4(h[0], h[1], h[2], h[3]);
             }
-            qs = fabsf(A.scale_log2) * kv8_unit<FMT>() * pow2i(e);
+            if (half == 0) {
+                reinterpret_cast<float *>(smem + M::kRows)[r] = fabsf(A.scale_log2) * kv8_unit<FMT>() * pow2i(e);
+                reinterpret_cast<int *>(smem + M::kRows)[2 * kTlRows + r] = W.seq_pos + tok;
+            }
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kBarQ));
+        if (!warp_wait(bar(kBarQ), 0)) failed = true;            // (the rows of a warp came through others)
 
-        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        const uint32_t t_s = t_lane + qt * kTlKeys, t_o = t_lane + 2 * kTlKeys + qt * D;
-        const int qpos0 = seq_pos + (pair0 + qt * kTlRows) / A.group;          // smallest and largest position of this tile
-        const int qpos1 = seq_pos + min(pair0 + pairs - 1, pair0 + qt * kTlRows + kTlRows - 1) / A.group;
-        float m = -INFINITY, l = 0.f;
-        if (qt < n_q) {
-            for (int i = 0; i < n_tiles; ++i) {
-                if (!warp_wait(bar(kBarScales + (i & 3)), (i >> 2) & 1) || !warp_wait(bar(kBarS + qt), i & 1)) { failed = true; break; }
+        const uint32_t t_lane = W.tmem + ((uint32_t)row0 << 16), t_o = t_lane + 4 * kTlKeys + qt * D;
+        // the tile's smallest and largest position
+        const int qpos0 = W.seq_pos + (W.pair0 + qt * kTlRows) / A.group;
+        const int qpos1 = W.seq_pos + (W.pair0 + min(W.pairs, qt * kTlRows + kTlRows) - 1) / A.group;
+        const int n_tiles = W.n_tiles;
+        float m[4], qs[4];
+        uint64_t l2[4];
+        int pos[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int r = qt * kTlRows + row0 + 8 * q + gi;
+            m[q] = -INFINITY;
+            l2[q] = 0;
+            qs[q] = reinterpret_cast<const float *>(smem + M::kRows)[r];
+            pos[q] = reinterpret_cast<const int *>(smem + M::kRows)[2 * kTlRows + r];
+        }
+        if (qt < W.n_q) {
+            for (int i = 0; i < n_tiles && !failed; ++i) {
+                if (!warp_wait(bar(kBarScales + (i & 7)), (i >> 3) & 1) || !warp_wait(bar(kBarS + qt * 2 + (i & 1)), (i >> 1) & 1)) {
+                    failed = true;
+                    break;
+                }
                 tc_fence_after_sync();
-                const unsigned char *stage = smem + M::kScales + (i & 3) * M::kStage;
-                const float *ks = reinterpret_cast<const float *>(stage), *vs = ks + 128;
-                const int *first = reinterpret_cast<const int *>(stage + 1024);
-                const int t0 = first[8];
-                const float turn = reinterpret_cast<const float *>(stage + 1024)[9];
+                const uint32_t t_s = t_lane + (qt * 2 + (i & 1)) * kTlKeys;
+                uint32_t sv[2][2][16];                            // [32 columns][16 rows]
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) tmem_ld_frag_issue(t_s + c * 32 + ((uint32_t)(16 * h) << 16), sv[c][h]);
+                const unsigned char *stage = smem + M::kScales + (i & 7) * M::kStage;
+                const unsigned char *ks = stage + tj * 8, *vs = ks + M::kVs;   // pairs of columns 8 b + 2 tj, + 1
+                const int *first = reinterpret_cast<const int *>(stage + M::kFirst);
+                const int t0 = first[4];
+                const float turn = reinterpret_cast<const float *>(stage + M::kFirst)[5];
                 const bool whole = t0 >= 0 && t0 + kTlKeys - 1 <= qpos0 && (!A.window || t0 > qpos1 - A.window || t0 + kTlKeys - 1 < A.sinks);
-                // which of 32 columns this row sees, as bits
-                auto seen = [&](int c) -> uint32_t {
-                    uint32_t bits = 0;
+                // bit 2 b + x of seen[q]: row q of the lane sees column 8 b + 2 tj + x
+                uint32_t seen[4] = {0, 0, 0, 0};
+                if (!whole) {
+#pragma unroll 1
+                    for (int b = 7; b >= 0; --b) {
+                        const int t = first[b >> 1] + (b & 1) * 8 + 2 * tj;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int t = first[2 * c + h];
-                        if (t > pos) continue;
-                        // tokens t .. t + 15: those <= pos, and of them those > pos - window or < sinks
-                        uint32_t b = pos - t >= 15 ? 0xFFFFu : (2u << (pos - t)) - 1u;
-                        if (A.window) {
-                            const int cut = pos - A.window - t;                // bits 0 .. cut lie before the window
-                            const uint32_t in = cut >= 15 ? 0u : cut < 0 ? 0xFFFFu : ~((2u << cut) - 1u);
-                            const int left = A.sinks - t;                      // bits 0 .. left - 1 are sinks
-                            b &= in | (left >= 16 ? 0xFFFFu : left <= 0 ? 0u : (1u << left) - 1u);
+                        for (int q = 0; q < 4; ++q) {
+                            const bool s0 = t <= pos[q] && (!A.window || t > pos[q] - A.window || t < A.sinks);
+                            const bool s1 = t + 1 <= pos[q] && (!A.window || t + 1 > pos[q] - A.window || t + 1 < A.sinks);
+                            seen[q] = seen[q] << 2 | (uint32_t)s0 | (uint32_t)s1 << 1;
                         }
-                        bits |= (b & 0xFFFFu) << (16 * h);
-                    }
-                    return bits;
-                };
-                // ---- the row's largest score (before qs >= 0) ----
-                float top = -INFINITY;
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t sv[32];
-                    tmem_ld_32cols(t_s + c * 32, sv);
-                    const uint32_t bits = whole ? ~0u : seen(c);
-#pragma unroll
-                    for (int x = 0; x < 32; x += 4) {
-                        const float4 kk = *reinterpret_cast<const float4 *>(ks + c * 32 + x);
-                        float z0 = __uint_as_float(sv[x]) * kk.x, z1 = __uint_as_float(sv[x + 1]) * kk.y;
-                        float z2 = __uint_as_float(sv[x + 2]) * kk.z, z3 = __uint_as_float(sv[x + 3]) * kk.w;
-                        if (!whole) {
-                            if (!(bits >> x & 1)) z0 = -INFINITY;
-                            if (!(bits >> (x + 1) & 1)) z1 = -INFINITY;
-                            if (!(bits >> (x + 2) & 1)) z2 = -INFINITY;
-                            if (!(bits >> (x + 3) & 1)) z3 = -INFINITY;
-                        }
-                        top = fmaxf(top, fmaxf(fmaxf(z0, z1), fmaxf(z2, z3)));
                     }
                 }
-                top = top == -INFINITY ? top : top * qs;
-                const bool move = top > m + kTlLazy;
-                if (__any_sync(~0u, move) || turn != 1.f) {
-                    const float next = move ? top : m, f = (move ? ex2_approx(m - next) : 1.f) * turn;
-                    l *= move ? ex2_approx(m - next) : 1.f;
-                    m = next;
-                    if (i > 0) {                                  // O holds the tiles before this one: they are done (S was issued after)
-#pragma unroll 1
-                        for (int c = 0; c < D / 32; ++c) {
-                            uint32_t ov[32];
-                            tmem_ld_32cols(t_o + c * 32, ov);
+                tmem_ld_wait();
 #pragma unroll
-                            for (int x = 0; x < 32; ++x) ov[x] = __float_as_uint(__uint_as_float(ov[x]) * f);
-                            tmem_st_32cols(t_o + c * 32, ov);
-                        }
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) tmem_tie16(sv[c][h]);
+                // ---- scores times the keys' scales, and the rows' largest (before qs >= 0) ----
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int b = 0; b < 8; ++b) {
+                    const uint64_t kk = *reinterpret_cast<const uint64_t *>(ks + b * 32);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t *r = &sv[b >> 2][q >> 1][(b & 3) * 4 + (q & 1) * 2];
+                        const float2 z = unpack2(mul2(pack2(r[0], r[1]), kk));
+                        r[0] = __float_as_uint(z.x);
+                        r[1] = __float_as_uint(z.y);
+                    }
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int b = 0; b < 8; ++b)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x)
+                                if (!(seen[q] >> (2 * b + x) & 1)) sv[b >> 2][q >> 1][(b & 3) * 4 + (q & 1) * 2 + x] = 0xFF800000u;
+                }
+#pragma unroll
+                for (int b = 0; b < 8; ++b)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t *r = &sv[b >> 2][q >> 1][(b & 3) * 4 + (q & 1) * 2];
+                        top[q] = max3(top[q], __uint_as_float(r[0]), __uint_as_float(r[1]));
+                    }
+                bool move = false;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    top[q] = top[q] == -INFINITY ? top[q] : top[q] * qs[q];
+                    move |= top[q] > m[q] + kTlLazy;
+                }
+                if (__any_sync(~0u, move) || turn != 1.f) {
+                    float f[4];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        float x = top[q];
+                        x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
+                        x = fmaxf(x, __shfl_xor_sync(~0u, x, 2));
+                        const bool up = x > m[q] + kTlLazy;
+                        const float next = up ? x : m[q], g = up ? ex2_approx(m[q] - next) : 1.f;
+                        l2[q] = mul2(l2[q], pack2f(g, g));
+                        m[q] = next;
+                        f[q] = g * turn;
+                    }
+                    if (i > 0) {
+                        // O holds the steps before this one, and the last of them may still be running (the step before that
+                        // one with the same barrier is long done: the scores of step i - 1 were issued after it)
+                        if (!warp_wait(bar(kBarPV + qt * 2 + ((i - 1) & 1)), ((i - 1) >> 1) & 1)) { failed = true; break; }
+                        tc_fence_after_sync();
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll 1
+                            for (int c = 0; c < D; c += 32) {
+                                const uint32_t at = t_o + c + ((uint32_t)(16 * h) << 16);
+                                uint32_t ov[16];
+                                tmem_ld_frag_issue(at, ov);
+                                tmem_ld_wait();
+                                tmem_tie16(ov);
+#pragma unroll
+                                for (int x = 0; x < 16; ++x) ov[x] = __float_as_uint(__uint_as_float(ov[x]) * f[2 * h + ((x >> 1) & 1)]);
+                                tmem_st_frag_f32(at, ov);
+                            }
+                        tmem_st_wait();
                     }
                 }
                 // ---- weights, over the scores they come from ----
-                const uint64_t qs2 = pack2f(qs, qs), nm2 = pack2f(-m, -m);
-                uint64_t sum2 = 0;
+                auto weigh = [&](auto masked) {
+                    constexpr bool MASK = decltype(masked)::value;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t sv[32], hi[16], lo[16];
-                    tmem_ld_32cols(t_s + c * 32, sv);
-                    const uint32_t bits = whole ? ~0u : seen(c);
+                    for (int c = 0; c < 2; ++c) {
+                        uint32_t hi[2][8], lo[2][8];
 #pragma unroll
-                    for (int x = 0; x < 32; x += 4) {
-                        const ulonglong2 kk = *reinterpret_cast<const ulonglong2 *>(ks + c * 32 + x);
-                        const ulonglong2 vv = *reinterpret_cast<const ulonglong2 *>(vs + c * 32 + x);
+                        for (int b = 0; b < 4; ++b) {
+                            const uint64_t vv = *reinterpret_cast<const uint64_t *>(vs + (c * 4 + b) * 32);
 #pragma unroll
-                        for (int y = 0; y < 2; ++y) {
-                            const int at = x + 2 * y;
-                            const float2 z = unpack2(fma2(mul2(pack2(sv[at], sv[at + 1]), y ? kk.y : kk.x), qs2, nm2));
-                            float p0 = ex2_approx(z.x), p1 = ex2_approx(z.y);
-                            if (!whole) {
-                                if (!(bits >> at & 1)) p0 = 0.f;
-                                if (!(bits >> (at + 1) & 1)) p1 = 0.f;
-                            }
-                            const uint64_t pp = pack2f(p0, p1);
-                            sum2 = add2(sum2, pp);
-                            float2 w = unpack2(mul2(pp, y ? vv.y : vv.x));
-                            if (!whole) {                         // (a hidden token's scale may be anything)
-                                if (!(bits >> at & 1)) w.x = 0.f;
-                                if (!(bits >> (at + 1) & 1)) w.y = 0.f;
-                            }
-                            hi[at / 2] = pack_f16x2(w.x, w.y);
-                            if (SPLIT) {
-                                const float2 back = half2_bits_to_float2(hi[at / 2]);
-                                lo[at / 2] = pack_f16x2(w.x - back.x, w.y - back.y);
+                            for (int q = 0; q < 4; ++q) {
+                                const uint32_t *r = &sv[c][q >> 1][b * 4 + (q & 1) * 2];
+                                const float2 z = unpack2(fma2(pack2(r[0], r[1]), pack2f(qs[q], qs[q]), pack2f(-m[q], -m[q])));
+                                float p0 = ex2_approx(z.x), p1 = ex2_approx(z.y);
+                                const bool s0 = !MASK || (seen[q] >> (8 * c + 2 * b) & 1);
+                                const bool s1 = !MASK || (seen[q] >> (8 * c + 2 * b + 1) & 1);
+                                if (MASK) {
+                                    if (!s0) p0 = 0.f;
+                                    if (!s1) p1 = 0.f;
+                                }
+                                const uint64_t pp = pack2f(p0, p1);
+                                l2[q] = add2(l2[q], pp);
+                                uint64_t ww = mul2(pp, vv);
+                                if (MASK) {                       // (a hidden token's scale may be anything)
+                                    float2 w = unpack2(ww);
+                                    if (!s0) w.x = 0.f;
+                                    if (!s1) w.y = 0.f;
+                                    ww = pack2f(w.x, w.y);
+                                }
+                                const float2 w = unpack2(ww);
+                                uint32_t &h = hi[q >> 1][b * 2 + (q & 1)];
+                                h = pack_f16x2(w.x, w.y);
+                                if (SPLIT) {
+                                    const float2 back = half2_bits_to_float2(h);
+                                    const float2 rest = unpack2(fma2(pack2f(back.x, back.y), pack2f(-1.f, -1.f), ww));
+                                    lo[q >> 1][b * 2 + (q & 1)] = pack_f16x2(rest.x, rest.y);
+                                }
                             }
                         }
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint32_t to = t_s + c * 32 + ((uint32_t)(16 * h) << 16);
+                            if (SPLIT) tmem_st_frag32(to, hi[h], lo[h]);
+                            else tmem_st_frag16(to, hi[h]);
+                        }
                     }
-                    tmem_st_16cols_issue(t_s + c * 32, hi);
-                    if (SPLIT) tmem_st_16cols_issue(t_s + c * 32 + 16, lo);
-                }
-                const float2 sum = unpack2(sum2);
-                l += sum.x + sum.y;
+                };
+                if (whole) weigh(std::false_type()); else weigh(std::true_type());
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kBarP + qt));
+                if (lane == 0) mbar_arrive(bar(kBarP + qt * 2 + (i & 1)));
             }
             // ---- the result ----
-            if (!failed && n_tiles > 0 && !warp_wait(bar(kBarO), 0)) failed = true;
+            if (!failed && n_tiles > 0 && !warp_wait(bar(kBarO + qt), 0)) failed = true;
             tc_fence_after_sync();
             if (!failed) {
                 float sigma = 0.f;
-                if (n_tiles > 0) sigma = reinterpret_cast<const float *>(smem + M::kScales + ((n_tiles - 1) & 3) * M::kStage + 1024)[10];
-                const bool empty = l == 0.f;
-                const float inv = empty ? 0.f : 1.f / l * (kv8_unit<FMT>() / kTlWeightUnit) * sigma;
-                const float lse2 = empty ? -INFINITY : m + log2f(l);
-                const int64_t part = ((((int64_t)idx * P.hkv + kvh) * 2 + qt) * kTlRows + row) * A.splits + split;
-                uint16_t *op = static_cast<uint16_t *>(A.out) + (int64_t)(s.start + tok) * A.o_rs + (int64_t)head * A.o_hs;
-                float *pa = A.part_acc + part * D;
-#pragma unroll 1
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t ov[32];
-                    if (n_tiles > 0) tmem_ld_32cols(t_o + c * 32, ov);
+                if (n_tiles > 0) sigma = reinterpret_cast<const float *>(smem + M::kScales + ((n_tiles - 1) & 7) * M::kStage + M::kFirst)[6];
+                const int parts = W.parts;
+                float inv[4];
+                bool live[4];
+                uint16_t *op[4];
+                float *pa[4];
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) ov[x] = empty ? 0u : __float_as_uint(__uint_as_float(ov[x]) * inv);
-                    if (live && parts == 1) {
-#pragma unroll
-                        for (int x = 0; x < 32; x += 8) {
-                            uint32_t h[4];
-#pragma unroll
-                            for (int y = 0; y < 4; ++y)
-                                h[y] = float2_to_pair(__uint_as_float(ov[x + 2 * y]), __uint_as_float(ov[x + 2 * y + 1]), A.bf16);
-                            *reinterpret_cast<uint4 *>(op + c * 32 + x) = make_uint4(h[0], h[1], h[2], h[3]);
-                        }
-                    } else if (live) {
-#pragma unroll
-                        for (int x = 0; x < 32; x += 4)
-                            *reinterpret_cast<uint4 *>(pa + c * 32 + x) = make_uint4(ov[x], ov[x + 1], ov[x + 2], ov[x + 3]);
+                for (int q = 0; q < 4; ++q) {
+                    const float2 x = unpack2(l2[q]);
+                    float l = x.x + x.y;
+                    l += __shfl_xor_sync(~0u, l, 1);
+                    l += __shfl_xor_sync(~0u, l, 2);
+                    const bool empty = l == 0.f;
+                    inv[q] = empty ? 0.f : 1.f / l * (kv8_unit<FMT>() / kTlWeightUnit) * sigma;
+                    const float lse2 = empty ? -INFINITY : m[q] + log2f(l);
+                    const int r = qt * kTlRows + row0 + 8 * q + gi, pair = W.pair0 + r, tok = W.start + pair / A.group;
+                    const int head = (int)(blockIdx.x % P.hkv) * A.group + pair % A.group;
+                    live[q] = r < W.pairs;
+                    op[q] = static_cast<uint16_t *>(A.out) + (int64_t)tok * A.o_rs + (int64_t)head * A.o_hs + 2 * tj;
+                    const int64_t part = W.part0 + (int64_t)r * A.splits;
+                    pa[q] = A.part_acc + part * D + 2 * tj;
+                    if (live[q] && tj == 0) {
+                        if (parts > 1) A.part_lse[part] = lse2;
+                        else if (A.lse) A.lse[(int64_t)tok * A.hq + head] = lse2 * kLn2;
                     }
-                    __syncwarp();
                 }
-                if (live) {
-                    if (parts > 1) A.part_lse[part] = lse2;
-                    else if (A.lse) A.lse[(int64_t)(s.start + tok) * A.hq + head] = lse2 * kLn2;
-                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t ov[16];
+                        if (n_tiles > 0) {
+                            tmem_ld_frag_issue(t_o + c + ((uint32_t)(16 * h) << 16), ov);
+                            tmem_ld_wait();
+                            tmem_tie16(ov);
+                        }
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+#pragma unroll
+                            for (int y = 0; y < 2; ++y) {
+                                const int q = 2 * h + y;
+                                if (!live[q]) continue;
+                                const float u = n_tiles > 0 ? __uint_as_float(ov[b * 4 + y * 2]) * inv[q] : 0.f;
+                                const float v = n_tiles > 0 ? __uint_as_float(ov[b * 4 + y * 2 + 1]) * inv[q] : 0.f;
+                                if (parts == 1) *reinterpret_cast<uint32_t *>(op[q] + c + b * 8) = float2_to_pair(u, v, A.bf16);
+                                else *reinterpret_cast<float2 *>(pa[q] + c + b * 8) = make_float2(u, v);
+                            }
+                        __syncwarp();
+                    }
             }
         }
-    } else if (warp < 12) {
+    } else if (warp < 16) {
+        fewer_registers<kTlRegsConvert>();
         // ---------------------------------------------------------------------------------------- convert
-        const int cw = warp - 8;
-        constexpr int ROWS_IT = D == 128 ? 4 : 8, ITS = 32 / ROWS_IT;          // rows per 512 bytes, loads per thread and tile
-        // lane -> (row, 16 channels) such that eight neighbouring lanes write 128 different bytes of the swizzled operand
+        const bool keys = warp < 12;                                           // warps 8-11 keys, 12-15 values
+        const int cw = warp & 3;
+        constexpr int ROWS_IT = D == 128 ? 4 : 8, ITS = 16 / ROWS_IT;          // rows per 512 bytes, loads per thread and step
+        // A warp converts one block of each step. lane -> (row, 16 channels) such that eight neighbouring lanes write 128
+        // different bytes of the swizzled operand.
         const int grp = D == 128 ? (lane & 3) | ((lane >> 3) & 1) << 2 : lane & 3;
         const int rr = D == 128 ? ((lane >> 2) & 1) | ((lane >> 4) & 1) << 1 : lane >> 2;
-        const int32_t *table = P.table + (int64_t)s.b * P.table_width;
-        // lane's block of a tile: lane / 4. Its page (-1: nobody sees it).
-        auto page_of = [&](int i) -> int {
-            const int j = j0 + i * 8 + (lane >> 2);
-            if (i >= n_tiles || j >= j1) return -1;
-            const int page = table[span.token(j) / P.page_tokens];
-            if (page >= 0 && page < P.n_pages) return page;
-            kv8_report(P, H1B_ERR_BOUNDS);
-            return -1;
+        const uint8_t *codes = (keys ? P.k : P.v) + rr * D + grp * 16;
+        const float *scales = (keys ? P.ks : P.vs) + (lane & 3) * 4;
+        const int32_t *table = P.table + (int64_t)W.seq * P.table_width;
+        const int kvh = blockIdx.x % P.hkv, n_tiles = W.n_tiles;
+        // Lanes 4 x .. 4 x + 3 look after block x % 4 of a step: its first token, its entry of the table (asked for two steps
+        // ahead, looked at one ahead), and the scales of tokens 4 (lane % 4) .. + 3 of it.
+        struct Step {
+            uint4 r[ITS];
+            float4 sc;
+            int t;
         };
-        auto place_of = [&](int i, int page) -> int64_t {                      // token slot of the lane's block, or -1
-            if (page < 0) return -1;
-            const int t = span.token(j0 + i * 8 + (lane >> 2));
-            return ((int64_t)page * P.hkv + kvh) * P.page_tokens + t % P.page_tokens;
+        int t_next, in_page, page;
+        auto look_up = [&](int i) {
+            const int j = W.j0 + i * kTlBlocks + ((lane >> 2) & 3);
+            t_next = i < n_tiles && j < W.j1 ? (j < W.sink_blocks ? j : W.first + j - W.sink_blocks) * kKv8Block : kTlHidden;
+            if (t_next == kTlHidden) return;
+            const int col = t_next / P.page_tokens;
+            in_page = t_next - col * P.page_tokens;
+            page = table[col];
         };
-        auto load = [&](const uint8_t *base, int64_t place, uint4 (&r)[ITS]) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {                                      // the warp's rows are two of the tile's blocks
-                const int64_t at = __shfl_sync(~0u, place, (2 * cw + h) * 4);
-#pragma unroll
-                for (int it = 0; it < ITS / 2; ++it)
-                    r[h * (ITS / 2) + it] = at < 0 ? make_uint4(0, 0, 0, 0)
-                                                   : *reinterpret_cast<const uint4 *>(base + (at + it * ROWS_IT + rr) * D + grp * 16);
+        auto load = [&](Step &x) {                                              // what look_up() was last asked for
+            x.t = t_next;
+            if (x.t != kTlHidden && (page < 0 || page >= P.n_pages)) {
+                kv8_report(P, H1B_ERR_BOUNDS);
+                x.t = kTlHidden;
             }
-        };
-        auto convert = [&](unsigned char *dst, const uint4 (&r)[ITS]) {
+            const int64_t place = x.t == kTlHidden ? -1 : ((int64_t)page * P.hkv + kvh) * P.page_tokens + in_page;
+            x.sc = place < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcg(reinterpret_cast<const float4 *>(scales + place));
+            const int64_t at = __shfl_sync(~0u, place, cw * 4);
+            const uint8_t *src = codes + at * D;
 #pragma unroll
-            for (int it = 0; it < ITS; ++it) {
-                const int rw = 32 * cw + it * ROWS_IT + rr, slab = grp >> 2, c0 = (grp & 3) * 2;
-                uint32_t a[8];
-                kv8_codes4<FMT>(r[it].x, a[0], a[1]);
-                kv8_codes4<FMT>(r[it].y, a[2], a[3]);
-                kv8_codes4<FMT>(r[it].z, a[4], a[5]);
-                kv8_codes4<FMT>(r[it].w, a[6], a[7]);
-                unsigned char *line = dst + slab * 16384 + rw * 128;
-                *reinterpret_cast<uint4 *>(line + ((c0 ^ (rw & 7)) << 4)) = make_uint4(a[0], a[1], a[2], a[3]);
-                *reinterpret_cast<uint4 *>(line + (((c0 + 1) ^ (rw & 7)) << 4)) = make_uint4(a[4], a[5], a[6], a[7]);
-            }
+            for (int it = 0; it < ITS; ++it)
+                x.r[it] = at < 0 ? make_uint4(0, 0, 0, 0) : __ldcg(reinterpret_cast<const uint4 *>(src + it * ROWS_IT * D));
         };
-        auto load_scales = [&](const float *base, int64_t place) -> float4 {  // lane's four tokens: block lane / 4, 4 (lane % 4) ..
-            return place < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4 *>(base + place + (lane & 3) * 4);
-        };
-        uint4 kr[ITS], vr[ITS];
         float sigma = 0.f;
-        int page = page_of(0), page_next = page_of(1);
-        int64_t place = place_of(0, page);
-        load(P.k, place, kr);
-        float4 ks = load_scales(P.ks, place), vs = load_scales(P.vs, place);
-        for (int i = 0; i < n_tiles; ++i) {
-            const int st = i & 1;
-            load(P.v, place, vr);
-            // scales of the tile's 128 tokens (every warp has all of them), those that no row sees cleared
-            const int jb = j0 + i * 8 + (lane >> 2), t = jb < j1 ? span.token(jb) : kTlHidden;
+        auto step = [&](int i, Step &x) -> bool {
+            const int st = i & (kTlStages - 1);
+            // Scale stage i % 8 was last read by the softmax warps in step i - 8. Keys: the wait below, made before anything is
+            // written, says that the scores of step i - 4 are done, which were issued after the weights of step i - 6. Values:
+            // the wait of step i - 1 said that step i - 5's weights had been contracted.
+            if (keys && i >= kTlStages && !warp_wait(bar(kBarKFree + st), ((i / kTlStages) - 1) & 1)) return false;
+            unsigned char *stage = smem + M::kScales + (i & 7) * M::kStage;
+            const int t = x.t;
             {
-                float *kf = &ks.x, *vf = &vs.x;
-                float mx = 0.f;
+                float *f = &x.sc.x;
+                const int lo = W.lo, hi = W.hi, sinks = W.sinks;
 #pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const int tt = t + (lane & 3) * 4 + x;
-                    if (!(tt <= span.hi && (tt >= span.lo || tt < span.sinks))) kf[x] = vf[x] = 0.f;
-                    mx = fmaxf(mx, vf[x] <= 3.402823466e38f ? vf[x] : 0.f);
+                for (int y = 0; y < 4; ++y) {                                   // what no row sees may be anything
+                    const int tt = t + (lane & 3) * 4 + y;
+                    if (!(tt <= hi && (tt >= lo || tt < sinks))) f[y] = 0.f;
                 }
+            }
+            if (keys) {
+                if (lane < 16 && (lane >> 2) == cw) *reinterpret_cast<float4 *>(stage + lane * 16) = x.sc;    // this warp's block
+                const int t_first = __shfl_sync(~0u, t, 0), t_last = __shfl_sync(~0u, t, 12);
+                const bool row = __all_sync(~0u, t != kTlHidden) && t_last - t_first == kTlKeys - 16;
+                if (cw == 0) {
+                    if (lane < 16 && (lane & 3) == 0) *reinterpret_cast<int *>(stage + M::kFirst + lane) = t;
+                    if (lane == 0) *reinterpret_cast<int *>(stage + M::kFirst + 16) = row ? t_first : -1;
+                }
+            } else {
+                float mx = 0.f;                                                 // every warp has all 64 scales
+                const float *f = &x.sc.x;
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, o));
+                for (int y = 0; y < 4; ++y) mx = fmaxf(mx, f[y] <= 3.402823466e38f ? f[y] : 0.f);
                 float turn = 1.f;
-                if (mx > 4.f * sigma) {
-                    const float next = pow2i(clampi((int)(__float_as_uint(mx) >> 23) - 126, -117, 126));   // > mx
+                if (__any_sync(~0u, mx > 4.f * sigma)) {
+#pragma unroll
+                    for (int o = 1; o < 16; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, o));
+                    const float next = pow2i(clampi((int)(__float_as_uint(mx) >> 23) - 126, -117, 126));       // > mx
                     turn = sigma / next;
                     sigma = next;
                 }
                 const float g = sigma > 0.f ? kTlWeightUnit / sigma : 0.f;
-                // stage i % 4: its last readers were the softmax warps of tile i - 4, whose weights were contracted before
-                // the scores of tile i - 2, which the wait below (or, before it, tile i - 1's) has seen completed
-                if (i >= 2 && !warp_wait(bar(kBarKFree + st), ((i >> 1) - 1) & 1)) { failed = true; break; }
-                unsigned char *stage = smem + M::kScales + (i & 3) * M::kStage;
-                if ((lane >> 3) == cw) {                                       // this warp's 32 tokens
-                    *reinterpret_cast<float4 *>(stage + lane * 16) = ks;
-                    *reinterpret_cast<float4 *>(stage + 512 + lane * 16) = make_float4(vs.x * g, vs.y * g, vs.z * g, vs.w * g);
+                if (lane < 16 && (lane >> 2) == cw)
+                    *reinterpret_cast<float4 *>(stage + M::kVs + lane * 16) = make_float4(x.sc.x * g, x.sc.y * g, x.sc.z * g, x.sc.w * g);
+                if (cw == 0 && lane == 0) {
+                    *reinterpret_cast<float *>(stage + M::kFirst + 20) = turn;
+                    *reinterpret_cast<float *>(stage + M::kFirst + 24) = sigma;
                 }
-                const int shown = page >= 0 ? t : kTlHidden;
-                const int t_first = __shfl_sync(~0u, shown, 0), t_last = __shfl_sync(~0u, shown, 28);
-                const bool row = __all_sync(~0u, shown != kTlHidden) && t_last - t_first == 112;
-                if (cw == 0) {
-                    if ((lane & 3) == 0) *reinterpret_cast<int *>(stage + 1024 + lane) = shown;
-                    if (lane == 0) {
-                        *reinterpret_cast<int *>(stage + 1024 + 32) = row ? t_first : -1;
-                        *reinterpret_cast<float *>(stage + 1024 + 36) = turn;
-                        *reinterpret_cast<float *>(stage + 1024 + 40) = sigma;
-                    }
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(kBarScales + (i & 3)));
             }
-            convert(smem + M::kK + st * M::kKV1, kr);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kBarScales + (i & 7)));
+            if (!keys && i >= kTlStages && !warp_wait(bar(kBarVFree + st), ((i / kTlStages) - 1) & 1)) return false;
+            unsigned char *line = smem + (keys ? M::kK : M::kV) + st * M::kKV1 + (grp >> 2) * (kTlKeys * 128) + (16 * cw + rr) * 128;
+#pragma unroll
+            for (int it = 0; it < ITS; ++it) {
+                const int rw = it * ROWS_IT + rr, c0 = (grp & 3) * 2;          // (row % 8: the block's first row is a multiple of 16)
+                uint32_t a[8];
+                kv8_codes4<FMT>(x.r[it].x, a[0], a[1]);
+                kv8_codes4<FMT>(x.r[it].y, a[2], a[3]);
+                kv8_codes4<FMT>(x.r[it].z, a[4], a[5]);
+                kv8_codes4<FMT>(x.r[it].w, a[6], a[7]);
+                *reinterpret_cast<uint4 *>(line + it * ROWS_IT * 128 + ((c0 ^ (rw & 7)) << 4)) = make_uint4(a[0], a[1], a[2], a[3]);
+                *reinterpret_cast<uint4 *>(line + it * ROWS_IT * 128 + (((c0 + 1) ^ (rw & 7)) << 4)) = make_uint4(a[4], a[5], a[6], a[7]);
+            }
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kBarKFull + st));
-            page = page_next;
-            page_next = page_of(i + 2);
-            place = place_of(i + 1, page);
-            if (i + 1 < n_tiles) {
-                load(P.k, place, kr);
-                ks = load_scales(P.ks, place);
-                vs = load_scales(P.vs, place);
-            }
-            if (i >= 2 && !warp_wait(bar(kBarVFree + st), ((i >> 1) - 1) & 1)) { failed = true; break; }
-            convert(smem + M::kV + st * M::kKV1, vr);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kBarVFull + st));
-        }
-    } else if (lane == 0 && n_tiles > 0) {
+            if (lane == 0) mbar_arrive(bar((keys ? kBarKFull : kBarVFull) + st));
+            load(x);                                                           // step i + 1
+            look_up(i + 2);
+            return true;
+        };
+        Step now;
+        look_up(0);
+        load(now);
+        look_up(1);
+#pragma unroll 1
+        for (int i = 0; i < n_tiles && !failed; ++i) failed = !step(i, now);
+    } else {
+        fewer_registers<kTlRegsIssue>();
         // ---------------------------------------------------------------------------------------- issue
-        const uint32_t idesc_s = umma_idesc_f16_m128(kTlKeys), idesc_o = umma_idesc_f16_m128(D) | 1u << 16;   // B: channels contiguous
-        auto scores = [&](int qt, int i) {
+        // A thread for each of the two tiles: a wait that need not wait still takes it some 200 cycles, and one thread for
+        // both had no time left to keep the tensor cores busy.
+        const int qt = warp - 16;
+        if (qt < W.n_q && lane == 0 && W.n_tiles > 0) {
+            const uint32_t s_at = W.tmem + qt * 2 * kTlKeys, o_at = W.tmem + 4 * kTlKeys + qt * D;
+            const int n_tiles = W.n_tiles;
+            const uint32_t idesc_s = umma_idesc_f16_m128(kTlKeys), idesc_o = umma_idesc_f16_m128(D) | 1u << 16;   // B: channels contiguous
+            const uint32_t q_lo = desc_lo(sm + M::kQ + qt * M::kQ1, 16), k_lo = desc_lo(sm + M::kK, 16);
+            const uint32_t v_lo = desc_lo(sm + M::kV, kTlKeys * 128);
+            auto wait = [&](int b, uint32_t parity) {
+                if (!failed && !wait_phase(bar(b), parity)) failed = true;
+                return !failed;
+            };
+            auto scores = [&](int i) {
+                if (!wait(kBarKFull + (i & (kTlStages - 1)), (i / kTlStages) & 1)) return;
+                tc_fence_after_sync();
+                const uint32_t k = k_lo + (i & (kTlStages - 1)) * (M::kKV1 >> 4), to = s_at + (i & 1) * kTlKeys;
 #pragma unroll
-            for (int ks = 0; ks < D / 16; ++ks) {
-                const uint32_t off = (ks >> 2) * 16384 + (ks & 3) * 32;
-                umma_f16(tmem + qt * kTlKeys, umma_desc_k_sw128(sm + M::kQ + qt * M::kQ1 + off),
-                         umma_desc_k_sw128(sm + M::kK + (i & 1) * M::kKV1 + off), idesc_s, ks ? 1u : 0u);
-            }
-            umma_commit(bar(kBarS + qt));
-        };
-        auto values = [&](int qt, int i) {
-            const uint32_t v = sm + M::kV + (i & 1) * M::kKV1, p = tmem + qt * kTlKeys, o = tmem + 2 * kTlKeys + qt * D;
-#pragma unroll
-            for (int ks = 0; ks < kTlKeys / 16; ++ks) {
-                umma_f16_ta(o, p + weight_column(ks), umma_desc_mn_sw128(v + ks * 2048), idesc_o, (i | ks) ? 1u : 0u);
-                if (SPLIT) umma_f16_ta(o, p + weight_column(ks) + 16, umma_desc_mn_sw128(v + ks * 2048), idesc_o, 1u);
-            }
-        };
-        auto wait = [&](int b, uint32_t parity) {
-            if (!failed && !mbar_wait_bounded(bar(b), parity, kTlWaitNs)) failed = true;
-            return !failed;
-        };
-        if (wait(kBarQ, 0) && wait(kBarKFull, 0)) {
-            tc_fence_after_sync();
-            for (int qt = 0; qt < n_q; ++qt) scores(qt, 0);
-            umma_commit(bar(kBarKFree));
+                for (int ks = 0; ks < D / 16; ++ks)
+                    mma_ss(to, q_lo + (ks >> 2) * (kTlRows * 128 >> 4) + (ks & 3) * 2, k + (ks >> 2) * (kTlKeys * 128 >> 4) + (ks & 3) * 2,
+                           idesc_s, ks != 0);
+                umma_commit(bar(kBarS + qt * 2 + (i & 1)));
+                umma_commit(bar(kBarKFree + (i & (kTlStages - 1))));
+            };
+            // Scores run two steps ahead of the values: step i + 2's go where step i's weights were, after the contraction that
+            // reads those (this thread issues both, and they execute in order).
+            if (wait(kBarQ, 0))
+                for (int i = 0; i < 2 && i < n_tiles && !failed; ++i) scores(i);
             for (int i = 0; i < n_tiles && !failed; ++i) {
-                if (!wait(kBarVFull + (i & 1), (i >> 1) & 1)) break;
-                for (int qt = 0; qt < n_q; ++qt) {
-                    if (!wait(kBarP + qt, i & 1)) break;
-                    tc_fence_after_sync();
-                    values(qt, i);
-                    if (qt == n_q - 1) umma_commit(bar(kBarVFree + (i & 1)));
-                    if (i + 1 < n_tiles) {
-                        if (qt == 0 && !wait(kBarKFull + ((i + 1) & 1), ((i + 1) >> 1) & 1)) break;
-                        tc_fence_after_sync();
-                        scores(qt, i + 1);
-                        if (qt == n_q - 1) umma_commit(bar(kBarKFree + ((i + 1) & 1)));
-                    }
+                const int st = i & (kTlStages - 1);
+                if (!wait(kBarVFull + st, (i / kTlStages) & 1) || !wait(kBarP + qt * 2 + (i & 1), (i >> 1) & 1)) break;
+                tc_fence_after_sync();
+                const uint32_t v = v_lo + st * (M::kKV1 >> 4), p = s_at + (i & 1) * kTlKeys;
+#pragma unroll
+                for (int ks = 0; ks < kTlKeys / 16; ++ks) {
+                    mma_ts(o_at, p + weight_column(ks), v + ks * (2048 >> 4), idesc_o, ks != 0 || i != 0);
+                    if (SPLIT) mma_ts(o_at, p + weight_column(ks) + 16, v + ks * (2048 >> 4), idesc_o, true);
                 }
+                umma_commit(bar(kBarPV + qt * 2 + (i & 1)));
+                umma_commit(bar(kBarVFree + st));
+                if (i + 2 < n_tiles) scores(i + 2);
             }
+            umma_commit(bar(kBarO + qt));
+            (void)wait_phase(bar(kBarO + qt), 0);  // nothing is in flight when the tensor memory is released
         }
-        umma_commit(bar(kBarO));
-        (void)mbar_wait_bounded(bar(kBarO), 0, kTlWaitNs);       // nothing is in flight when the tensor memory is released
     }
     if (failed) kv8_report(P, H1B_ERR_TIMEOUT);
     __syncwarp();
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 12) { tc_fence_after_sync(); tmem_dealloc(tmem, 512); }
+    if (warp == 16) { tc_fence_after_sync(); tmem_dealloc(W.tmem, 512); }
 }
 
 template <int D, int FMT, bool SPLIT>
@@ -520,7 +698,7 @@ cudaError_t launch_kv8_tiles(const Kv8Params &P, const Kv8Attn &A, int d, int fm
     else e = fmt == H1B_KV8_INT8 ? H1B_KV8_TILES(64, H1B_KV8_INT8) : H1B_KV8_TILES(64, H1B_KV8_E4M3);
 #undef H1B_KV8_TILES
     if (e != cudaSuccess || A.splits == 1) return e;
-    return launch_kv8_join(P, A, d, 2 * kTlRows, 8, 16, st);
+    return launch_kv8_join(P, A, d, 2 * kTlRows, kTlUnit, kTlMinBlocks, st);
 }
 
 }  // namespace h1b
