@@ -21,6 +21,8 @@ struct Kv8Params {
     int n_pages, hkv, page_tokens;
     int n_seqs, table_width, n_rows;
     int cap;                               // table_width * page_tokens
+    uint32_t page_mul;                     // block / (page_tokens / 16) = block * page_mul >> page_shift, exactly, for
+    int page_shift;                        // block < 2^26 (all that 2^30 tokens have)
 };
 
 struct Kv8Attn {
@@ -41,6 +43,11 @@ struct Kv8Attn {
 
 __device__ __forceinline__ void kv8_report(const Kv8Params &P, int code) {
     if (P.status) *P.status = code;        // any one of several stays: the host asks whether there was one
+}
+
+// The entry of a sequence's table that block `block` (of 16 tokens) lies in.
+__device__ __forceinline__ int kv8_page_of(const Kv8Params &P, int block) {
+    return (int)((uint64_t)(uint32_t)block * P.page_mul >> P.page_shift);
 }
 
 __device__ __forceinline__ int clampi(int x, int lo, int hi) { return min(max(x, lo), hi); }

@@ -86,6 +86,13 @@ Kv8Params params_of(const h1b_kv8_pool *p, const h1b_kv8_batch *b) {
     P.n_pages = p->n_pages; P.hkv = p->n_kv_heads; P.page_tokens = p->page_tokens;
     P.n_seqs = b->n_seqs; P.table_width = b->table_width; P.n_rows = b->n_rows;
     P.cap = b->table_width * p->page_tokens;
+    // d = page_tokens / 16 <= 2^26: with k = 26 + ceil(log2 d) and m = ceil(2^k / d), block * m exceeds block * 2^k / d by less
+    // than 2^26 * d / d = a unit of 2^k / 2^ceil(log2 d), which is too little to reach the next quotient
+    const uint32_t d = (uint32_t)(p->page_tokens / kKv8Block);
+    int log2d = 0;
+    while ((1u << log2d) < d) ++log2d;
+    P.page_shift = 26 + log2d;
+    P.page_mul = (uint32_t)(((1ull << P.page_shift) + d - 1) / d);
     return P;
 }
 

@@ -1,13 +1,14 @@
 // 8-bit pages: attention for many rows per sequence (prompts and chunks of them) on the 5th-generation tensor cores.
 //
-// One block of 18 warps takes 256 (row, head of the group) pairs of a sequence that share a KV head, as two tiles of 128
+// One block of 19 warps takes 256 (row, head of the group) pairs of a sequence that share a KV head, as two tiles of 128
 // pairs, and one part of the tokens they see, 64 tokens at a time (four blocks of 16, whichever blocks the span lists: sinks
 // and window need not be neighbours). The roles hand each other operands through mbarriers; nothing in the loop is
 // block-wide:
-//   warps 8-15   convert (four warps the keys, four the values): codes come from the pages in 16-byte loads, one step
-//                ahead in registers, become exact fp16 numbers ONCE for all 256 pairs and go to shared memory as matrix
-//                operands (four of each, 128-byte swizzle; keys K-major, values with the channels contiguous, so nothing
+//   warps 8-15   convert (four warps the keys, four the values): codes come from the pages in 16-byte copies, two
+//                steps ahead, become exact fp16 numbers ONCE for all 256 pairs and go to shared memory as matrix
+//                operands (three of each, 128-byte swizzle; keys K-major, values with the channels contiguous, so nothing
 //                is transposed);
+//   warp 18      brings the tokens' scales;
 //   warps 16, 17 issue the contractions of tile A and of tile B: S = Q K^T into tensor memory, O += P V with P read from
 //                tensor memory;
 //   warps 0-3    softmax of tile A, warps 4-7 of tile B, 32 rows a warp: scores S * ks * qs, the rows' references,
@@ -27,15 +28,15 @@ namespace h1b {
 namespace {
 
 constexpr int kTlRows = 128, kTlKeys = 64, kTlBlocks = kTlKeys / kKv8Block;
-constexpr int kTlThreads = 20 * 32;                            // warps 0-7 softmax, 8-15 convert, 16-17 issue; 18, 19 only
-                                                                // hand over their registers
-constexpr int kTlRegsLaunch = 96, kTlRegsSoftmax = 144, kTlRegsConvert = 64, kTlRegsIssue = 64;
+constexpr int kTlThreads = 20 * 32;                            // warps 0-7 softmax, 8-15 convert, 16-17 issue, 18 scales;
+                                                                // 19 only hands over its registers
+constexpr int kTlRegsLaunch = 96, kTlRegsSoftmax = 152, kTlRegsConvert = 56, kTlRegsIssue = 64;
 static_assert(256 * kTlRegsSoftmax + 256 * kTlRegsConvert + 128 * kTlRegsIssue <= kTlThreads * kTlRegsLaunch,
               "more registers than a block is launched with");
 constexpr float kTlLazy = 4.f, kTlWeightUnit = 512.f;
 constexpr int kTlHidden = 1 << 30;                             // "first token" of a block that nobody sees: beyond every position
 constexpr int kTlUnit = kTlBlocks, kTlMinBlocks = 16;         // a part is whole steps, and 256 tokens at least
-constexpr int kTlStages = 4, kTlScaleStages = 8;
+constexpr int kTlStages = 3, kTlScaleStages = 4, kTlRawStages = 3;
 
 // What a block works on, in shared memory: each role reads what it needs where it needs it. (Kept in registers across the
 // roles' branches it was spilled, and a reload from local memory, whose lines the codes push out of the small L1, held up
@@ -48,16 +49,17 @@ struct TlWork {
 
 template <int D>
 struct TlSmem {
-    static constexpr int kQ1 = kTlRows * D * 2, kKV1 = kTlKeys * D * 2;
-    static constexpr int kQ = 0, kK = 2 * kQ1, kV = kK + kTlStages * kKV1, kScales = kV + kTlStages * kKV1;
+    static constexpr int kQ1 = kTlRows * D * 2, kKV1 = kTlKeys * D * 2, kRaw1 = 2 * kTlKeys * D;
+    static constexpr int kQ = 0, kK = 2 * kQ1, kV = kK + kTlStages * kKV1, kRaw = kV + kTlStages * kKV1;
+    static constexpr int kScales = kRaw + kTlRawStages * kRaw1;
     // per scale stage: ks [64], vs / sigma [64], blocks' first tokens [4], {first token if all 64 are in a row, else -1; turn; sigma}
     static constexpr int kVs = kTlKeys * 4, kFirst = 2 * kTlKeys * 4, kStage = kFirst + 32;
     static constexpr int kRows = kScales + kTlScaleStages * kStage;              // qs [256], positions [256]
     static constexpr int kBars = kRows + 2 * kTlRows * 8;
     static constexpr int kTotal = kBars + 512 + 1024;            // + slack to align the operands to 1024 bytes
 };
-enum { kBarQ = 0, kBarKFull = 1, kBarKFree = 5, kBarVFull = 9, kBarVFree = 13, kBarScales = 17, kBarS = 25, kBarP = 29, kBarPV = 33,
-       kBarO = 37, kBarCount = 39 };
+enum { kBarQ = 0, kBarFull = 1, kBarKFree = 4, kBarVFree = 7, kBarScales = 10, kBarS = 14, kBarP = 18, kBarPV = 22, kBarO = 26,
+       kBarCount = 28 };
 
 __device__ __forceinline__ uint64_t pack2(uint32_t lo, uint32_t hi) {
     uint64_t r;
@@ -145,6 +147,11 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity) {
     return false;
 }
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity) { return __all_sync(~0u, wait_phase(bar, parity)); }
+// Two at once (a look takes 100 cycles and more when shared memory is busy).
+__device__ __forceinline__ bool warp_wait2(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1) {
+    const bool a = mbar_try_wait(bar0, parity0), b = mbar_try_wait(bar1, parity1);
+    return __all_sync(~0u, a && b) || (warp_wait(bar0, parity0) && warp_wait(bar1, parity1));
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -205,11 +212,9 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
     if (tid == 0) {
         for (int i = 0; i < kBarCount; ++i) {                    // arrivals: one a warp, or one commit
             int n = 1;
-            if (i == kBarQ) n = 8;
-            else if (i >= kBarScales && i < kBarS) n = 8;
+            if (i == kBarQ || (i >= kBarFull && i < kBarKFree)) n = 8;
             else if (i >= kBarP && i < kBarPV) n = 4;
-            else if ((i >= kBarKFull && i < kBarKFree) || (i >= kBarVFull && i < kBarVFree)) n = 4;
-            else if ((i >= kBarKFree && i < kBarVFull) || (i >= kBarVFree && i < kBarScales)) n = W.n_q;
+            else if (i >= kBarKFree && i < kBarScales) n = W.n_q;
             mbar_init(bar(i), n);
         }
         mbar_fence_init();
@@ -277,20 +282,18 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
         const int qpos0 = W.seq_pos + (W.pair0 + qt * kTlRows) / A.group;
         const int qpos1 = W.seq_pos + (W.pair0 + min(W.pairs, qt * kTlRows + kTlRows) - 1) / A.group;
         const int n_tiles = W.n_tiles;
-        float m[4], qs[4];
-        uint64_t l2[4];
-        int pos[4];
+        uint64_t qs2[4], nm2[4], l2[4];                          // of each row, twice: qs, -m, and the two halves of the sum
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const int r = qt * kTlRows + row0 + 8 * q + gi;
-            m[q] = -INFINITY;
+            const float qs = reinterpret_cast<const float *>(smem + M::kRows)[qt * kTlRows + row0 + 8 * q + gi];
+            qs2[q] = pack2f(qs, qs);
+            nm2[q] = pack2f(INFINITY, INFINITY);
             l2[q] = 0;
-            qs[q] = reinterpret_cast<const float *>(smem + M::kRows)[r];
-            pos[q] = reinterpret_cast<const int *>(smem + M::kRows)[2 * kTlRows + r];
         }
+        const int *row_pos = reinterpret_cast<const int *>(smem + M::kRows) + 2 * kTlRows + qt * kTlRows + row0 + gi;
         if (qt < W.n_q) {
             for (int i = 0; i < n_tiles && !failed; ++i) {
-                if (!warp_wait(bar(kBarScales + (i & 7)), (i >> 3) & 1) || !warp_wait(bar(kBarS + qt * 2 + (i & 1)), (i >> 1) & 1)) {
+                if (!warp_wait2(bar(kBarScales + (i & 3)), (i >> 2) & 1, bar(kBarS + qt * 2 + (i & 1)), (i >> 1) & 1)) {
                     failed = true;
                     break;
                 }
@@ -301,7 +304,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) tmem_ld_frag_issue(t_s + c * 32 + ((uint32_t)(16 * h) << 16), sv[c][h]);
-                const unsigned char *stage = smem + M::kScales + (i & 7) * M::kStage;
+                const unsigned char *stage = smem + M::kScales + (i & 3) * M::kStage;
                 const unsigned char *ks = stage + tj * 8, *vs = ks + M::kVs;   // pairs of columns 8 b + 2 tj, + 1
                 const int *first = reinterpret_cast<const int *>(stage + M::kFirst);
                 const int t0 = first[4];
@@ -315,8 +318,9 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                         const int t = first[b >> 1] + (b & 1) * 8 + 2 * tj;
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const bool s0 = t <= pos[q] && (!A.window || t > pos[q] - A.window || t < A.sinks);
-                            const bool s1 = t + 1 <= pos[q] && (!A.window || t + 1 > pos[q] - A.window || t + 1 < A.sinks);
+                            const int pos = row_pos[8 * q];
+                            const bool s0 = t <= pos && (!A.window || t > pos - A.window || t < A.sinks);
+                            const bool s1 = t + 1 <= pos && (!A.window || t + 1 > pos - A.window || t + 1 < A.sinks);
                             seen[q] = seen[q] << 2 | (uint32_t)s0 | (uint32_t)s1 << 1;
                         }
                     }
@@ -355,23 +359,21 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                         const uint32_t *r = &sv[b >> 2][q >> 1][(b & 3) * 4 + (q & 1) * 2];
                         top[q] = max3(top[q], __uint_as_float(r[0]), __uint_as_float(r[1]));
                     }
-                bool move = false;
+                float over = -INFINITY;                           // how far a score lies above its row's reference
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    top[q] = top[q] == -INFINITY ? top[q] : top[q] * qs[q];
-                    move |= top[q] > m[q] + kTlLazy;
-                }
-                if (__any_sync(~0u, move) || turn != 1.f) {
+                for (int q = 0; q < 4; ++q) over = fmaxf(over, fmaf(top[q], unpack2(qs2[q]).x, unpack2(nm2[q]).x));
+                if (__any_sync(~0u, over > kTlLazy) || turn != 1.f) {
                     float f[4];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        float x = top[q];
+                        const float m = -unpack2(nm2[q]).x;
+                        float x = top[q] == -INFINITY ? top[q] : top[q] * unpack2(qs2[q]).x;
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 2));
-                        const bool up = x > m[q] + kTlLazy;
-                        const float next = up ? x : m[q], g = up ? ex2_approx(m[q] - next) : 1.f;
+                        const bool up = x > m + kTlLazy;
+                        const float g = up ? ex2_approx(m - x) : 1.f;
                         l2[q] = mul2(l2[q], pack2f(g, g));
-                        m[q] = next;
+                        if (up) nm2[q] = pack2f(-x, -x);
                         f[q] = g * turn;
                     }
                     if (i > 0) {
@@ -407,7 +409,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
 #pragma unroll
                             for (int q = 0; q < 4; ++q) {
                                 const uint32_t *r = &sv[c][q >> 1][b * 4 + (q & 1) * 2];
-                                const float2 z = unpack2(fma2(pack2(r[0], r[1]), pack2f(qs[q], qs[q]), pack2f(-m[q], -m[q])));
+                                const float2 z = unpack2(fma2(pack2(r[0], r[1]), qs2[q], nm2[q]));
                                 float p0 = ex2_approx(z.x), p1 = ex2_approx(z.y);
                                 const bool s0 = !MASK || (seen[q] >> (8 * c + 2 * b) & 1);
                                 const bool s1 = !MASK || (seen[q] >> (8 * c + 2 * b + 1) & 1);
@@ -453,7 +455,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
             tc_fence_after_sync();
             if (!failed) {
                 float sigma = 0.f;
-                if (n_tiles > 0) sigma = reinterpret_cast<const float *>(smem + M::kScales + ((n_tiles - 1) & 7) * M::kStage + M::kFirst)[6];
+                if (n_tiles > 0) sigma = reinterpret_cast<const float *>(smem + M::kScales + ((n_tiles - 1) & 3) * M::kStage + M::kFirst)[6];
                 const int parts = W.parts;
                 float inv[4];
                 bool live[4];
@@ -467,7 +469,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                     l += __shfl_xor_sync(~0u, l, 2);
                     const bool empty = l == 0.f;
                     inv[q] = empty ? 0.f : 1.f / l * (kv8_unit<FMT>() / kTlWeightUnit) * sigma;
-                    const float lse2 = empty ? -INFINITY : m[q] + log2f(l);
+                    const float lse2 = empty ? -INFINITY : log2f(l) - unpack2(nm2[q]).x;
                     const int r = qt * kTlRows + row0 + 8 * q + gi, pair = W.pair0 + r, tok = W.start + pair / A.group;
                     const int head = (int)(blockIdx.x % P.hkv) * A.group + pair % A.group;
                     live[q] = r < W.pairs;
@@ -511,125 +513,143 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
         const int cw = warp & 3;
         constexpr int ROWS_IT = D == 128 ? 4 : 8, ITS = 16 / ROWS_IT;          // rows per 512 bytes, loads per thread and step
         // A warp converts one block of each step. lane -> (row, 16 channels) such that eight neighbouring lanes write 128
-        // different bytes of the swizzled operand.
+        // different bytes of the swizzled operand. The codes come to shared memory with asynchronous copies two steps ahead; a
+        // lane converts the very bytes that it copied, so nobody else has to know.
         const int grp = D == 128 ? (lane & 3) | ((lane >> 3) & 1) << 2 : lane & 3;
         const int rr = D == 128 ? ((lane >> 2) & 1) | ((lane >> 4) & 1) << 1 : lane >> 2;
-        const uint8_t *codes = (keys ? P.k : P.v) + rr * D + grp * 16;
-        const float *scales = (keys ? P.ks : P.vs) + (lane & 3) * 4;
+        const uint8_t *codes = (keys ? P.k : P.v) + (int64_t)(blockIdx.x % P.hkv) * P.page_tokens * D + rr * D + grp * 16;
         const int32_t *table = P.table + (int64_t)W.seq * P.table_width;
-        const int kvh = blockIdx.x % P.hkv, n_tiles = W.n_tiles;
-        // Lanes 4 x .. 4 x + 3 look after block x % 4 of a step: its first token, its entry of the table (asked for two steps
-        // ahead, looked at one ahead), and the scales of tokens 4 (lane % 4) .. + 3 of it.
-        struct Step {
-            uint4 r[ITS];
-            float4 sc;
-            int t;
-        };
-        int t_next, in_page, page;
+        const uint32_t raw = sm + M::kRaw + (warp - 8) * 16 * D + lane * 16;
+        const int n_tiles = W.n_tiles, j_first = W.j0 + cw, j1 = W.j1, sink_blocks = W.sink_blocks, skip = W.first - sink_blocks;
+        int offset = 0, page = -1;                                              // asked for last: the block's place in its page, the page
         auto look_up = [&](int i) {
-            const int j = W.j0 + i * kTlBlocks + ((lane >> 2) & 3);
-            t_next = i < n_tiles && j < W.j1 ? (j < W.sink_blocks ? j : W.first + j - W.sink_blocks) * kKv8Block : kTlHidden;
-            if (t_next == kTlHidden) return;
-            const int col = t_next / P.page_tokens;
-            in_page = t_next - col * P.page_tokens;
+            const int j = j_first + i * kTlBlocks;
+            page = -1;
+            if (j >= j1) return;
+            const int blk = j < sink_blocks ? j : j + skip, col = kv8_page_of(P, blk);
+            offset = blk * kKv8Block - col * P.page_tokens;
             page = table[col];
         };
-        auto load = [&](Step &x) {                                              // what look_up() was last asked for
-            x.t = t_next;
-            if (x.t != kTlHidden && (page < 0 || page >= P.n_pages)) {
-                kv8_report(P, H1B_ERR_BOUNDS);
-                x.t = kTlHidden;
-            }
-            const int64_t place = x.t == kTlHidden ? -1 : ((int64_t)page * P.hkv + kvh) * P.page_tokens + in_page;
-            x.sc = place < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : __ldcg(reinterpret_cast<const float4 *>(scales + place));
-            const int64_t at = __shfl_sync(~0u, place, cw * 4);
-            const uint8_t *src = codes + at * D;
+        auto fetch = [&](int stage) {                                           // the copies of the step looked up
+            const bool ok = page >= 0 && page < P.n_pages;                      // (a block that nobody sees: zeros)
+            const uint8_t *src = codes + ((int64_t)(ok ? page : 0) * P.hkv * P.page_tokens + offset) * D;
 #pragma unroll
             for (int it = 0; it < ITS; ++it)
-                x.r[it] = at < 0 ? make_uint4(0, 0, 0, 0) : __ldcg(reinterpret_cast<const uint4 *>(src + it * ROWS_IT * D));
+                cp_async_16(raw + stage * M::kRaw1 + it * 512, src + it * ROWS_IT * D, ok ? 16 : 0);
+            cp_async_commit();
         };
-        float sigma = 0.f;
-        auto step = [&](int i, Step &x) -> bool {
-            const int st = i & (kTlStages - 1);
-            // Scale stage i % 8 was last read by the softmax warps in step i - 8. Keys: the wait below, made before anything is
-            // written, says that the scores of step i - 4 are done, which were issued after the weights of step i - 6. Values:
-            // the wait of step i - 1 said that step i - 5's weights had been contracted.
-            if (keys && i >= kTlStages && !warp_wait(bar(kBarKFree + st), ((i / kTlStages) - 1) & 1)) return false;
-            unsigned char *stage = smem + M::kScales + (i & 7) * M::kStage;
-            const int t = x.t;
-            {
-                float *f = &x.sc.x;
-                const int lo = W.lo, hi = W.hi, sinks = W.sinks;
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {                                   // what no row sees may be anything
-                    const int tt = t + (lane & 3) * 4 + y;
-                    if (!(tt <= hi && (tt >= lo || tt < sinks))) f[y] = 0.f;
-                }
-            }
-            if (keys) {
-                if (lane < 16 && (lane >> 2) == cw) *reinterpret_cast<float4 *>(stage + lane * 16) = x.sc;    // this warp's block
-                const int t_first = __shfl_sync(~0u, t, 0), t_last = __shfl_sync(~0u, t, 12);
-                const bool row = __all_sync(~0u, t != kTlHidden) && t_last - t_first == kTlKeys - 16;
-                if (cw == 0) {
-                    if (lane < 16 && (lane & 3) == 0) *reinterpret_cast<int *>(stage + M::kFirst + lane) = t;
-                    if (lane == 0) *reinterpret_cast<int *>(stage + M::kFirst + 16) = row ? t_first : -1;
-                }
-            } else {
-                float mx = 0.f;                                                 // every warp has all 64 scales
-                const float *f = &x.sc.x;
-#pragma unroll
-                for (int y = 0; y < 4; ++y) mx = fmaxf(mx, f[y] <= 3.402823466e38f ? f[y] : 0.f);
-                float turn = 1.f;
-                if (__any_sync(~0u, mx > 4.f * sigma)) {
-#pragma unroll
-                    for (int o = 1; o < 16; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, o));
-                    const float next = pow2i(clampi((int)(__float_as_uint(mx) >> 23) - 126, -117, 126));       // > mx
-                    turn = sigma / next;
-                    sigma = next;
-                }
-                const float g = sigma > 0.f ? kTlWeightUnit / sigma : 0.f;
-                if (lane < 16 && (lane >> 2) == cw)
-                    *reinterpret_cast<float4 *>(stage + M::kVs + lane * 16) = make_float4(x.sc.x * g, x.sc.y * g, x.sc.z * g, x.sc.w * g);
-                if (cw == 0 && lane == 0) {
-                    *reinterpret_cast<float *>(stage + M::kFirst + 20) = turn;
-                    *reinterpret_cast<float *>(stage + M::kFirst + 24) = sigma;
-                }
-            }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kBarScales + (i & 7)));
-            if (!keys && i >= kTlStages && !warp_wait(bar(kBarVFree + st), ((i / kTlStages) - 1) & 1)) return false;
+        look_up(0);
+        fetch(0);
+        look_up(1);
+        fetch(1);
+        look_up(2);
+        int st = 0, phase = 1;                                                  // i % 3, and i / 3 - 1 as a parity
+#pragma unroll 1
+        for (int i = 0; i < n_tiles; ++i) {
+            fetch(st == 0 ? 2 : st - 1);                                        // step i + 2 into (i + 2) % 3, which was read in step i - 1
+            look_up(i + 3);
+            if (i >= kTlStages && !warp_wait(bar((keys ? kBarKFree : kBarVFree) + st), phase)) { failed = true; break; }
+            cp_async_wait_group<2>();                                           // this step's copies
             unsigned char *line = smem + (keys ? M::kK : M::kV) + st * M::kKV1 + (grp >> 2) * (kTlKeys * 128) + (16 * cw + rr) * 128;
+            const unsigned char *src = smem + (raw - sm) + st * M::kRaw1;
 #pragma unroll
             for (int it = 0; it < ITS; ++it) {
                 const int rw = it * ROWS_IT + rr, c0 = (grp & 3) * 2;          // (row % 8: the block's first row is a multiple of 16)
+                const uint4 r = *reinterpret_cast<const uint4 *>(src + it * 512);
                 uint32_t a[8];
-                kv8_codes4<FMT>(x.r[it].x, a[0], a[1]);
-                kv8_codes4<FMT>(x.r[it].y, a[2], a[3]);
-                kv8_codes4<FMT>(x.r[it].z, a[4], a[5]);
-                kv8_codes4<FMT>(x.r[it].w, a[6], a[7]);
+                kv8_codes4<FMT>(r.x, a[0], a[1]);
+                kv8_codes4<FMT>(r.y, a[2], a[3]);
+                kv8_codes4<FMT>(r.z, a[4], a[5]);
+                kv8_codes4<FMT>(r.w, a[6], a[7]);
                 *reinterpret_cast<uint4 *>(line + it * ROWS_IT * 128 + ((c0 ^ (rw & 7)) << 4)) = make_uint4(a[0], a[1], a[2], a[3]);
                 *reinterpret_cast<uint4 *>(line + it * ROWS_IT * 128 + (((c0 + 1) ^ (rw & 7)) << 4)) = make_uint4(a[4], a[5], a[6], a[7]);
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar((keys ? kBarKFull : kBarVFull) + st));
-            load(x);                                                           // step i + 1
-            look_up(i + 2);
-            return true;
-        };
-        Step now;
-        look_up(0);
-        load(now);
-        look_up(1);
-#pragma unroll 1
-        for (int i = 0; i < n_tiles && !failed; ++i) failed = !step(i, now);
+            if (lane == 0) mbar_arrive(bar(kBarFull + st));
+            if (++st == kTlStages) { st = 0; phase ^= 1; }
+        }
+        cp_async_wait_group<0>();
     } else {
         fewer_registers<kTlRegsIssue>();
         // ---------------------------------------------------------------------------------------- issue
         // A thread for each of the two tiles: a wait that need not wait still takes it some 200 cycles, and one thread for
         // both had no time left to keep the tensor cores busy.
         const int qt = warp - 16;
-        if (qt < W.n_q && lane == 0 && W.n_tiles > 0) {
+        if (warp == 18) {
+            // ------------------------------------------------------------------------------------ scales
+            // Lanes 4 x .. 4 x + 3 look after block x % 4 of a step: its first token, its page, and the scales of tokens
+            // 4 (lane % 4) .. + 3 of it, the keys' (lanes 0 - 15) or the values' (16 - 31). The table is read two steps ahead,
+            // the scales one.
+            const bool keys = lane < 16;
+            const float *scales = (keys ? P.ks : P.vs) + (int64_t)(blockIdx.x % P.hkv) * P.page_tokens + (lane & 3) * 4;
+            const int32_t *table = P.table + (int64_t)W.seq * P.table_width;
+            const int n_tiles = W.n_tiles, j_first = W.j0 + ((lane >> 2) & 3), j1 = W.j1, sink_blocks = W.sink_blocks, skip = W.first - sink_blocks;
+            const int lo = W.lo, hi = W.hi, sinks = W.sinks;
+            int t_next = kTlHidden, offset = 0, page = -1;
+            auto look_up = [&](int i) {
+                const int j = j_first + i * kTlBlocks;
+                t_next = kTlHidden;
+                if (j >= j1) return;
+                const int blk = j < sink_blocks ? j : j + skip, col = kv8_page_of(P, blk);
+                t_next = blk * kKv8Block;
+                offset = t_next - col * P.page_tokens;
+                page = table[col];
+            };
+            int t;
+            float4 sc;
+            auto fetch = [&]() {                                                // the scales of the step looked up
+                t = t_next;
+                if (t != kTlHidden && (page < 0 || page >= P.n_pages)) {
+                    kv8_report(P, H1B_ERR_BOUNDS);
+                    t = kTlHidden;
+                }
+                sc = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (t != kTlHidden) sc = __ldcg(reinterpret_cast<const float4 *>(scales + (int64_t)page * P.hkv * P.page_tokens + offset));
+            };
+            look_up(0);
+            fetch();
+            look_up(1);
+            float sigma = 0.f;
+            int st = 0, phase = 1;
+#pragma unroll 1
+            for (int i = 0; i < n_tiles; ++i) {
+                // Stage i % 4 was last read in step i - 4, whose weights had been contracted before those of step i - 3.
+                if (i >= kTlStages && !warp_wait(bar(kBarVFree + st), phase)) { failed = true; break; }
+                unsigned char *stage = smem + M::kScales + (i & 3) * M::kStage;
+                float *f = &sc.x;
+                float mx = 0.f;
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {                                   // what no row sees may be anything
+                    const int tt = t + (lane & 3) * 4 + y;
+                    if (!(tt <= hi && (tt >= lo || tt < sinks))) f[y] = 0.f;
+                    mx = fmaxf(mx, !keys && f[y] <= 3.402823466e38f ? f[y] : 0.f);
+                }
+                float turn = 1.f;                                               // old sigma / new sigma
+                if (__any_sync(~0u, mx > 4.f * sigma)) {
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, o));
+                    const float next = pow2i(clampi((int)(__float_as_uint(mx) >> 23) - 126, -117, 126));       // > mx
+                    turn = sigma / next;
+                    sigma = next;
+                }
+                const float g = keys ? 1.f : sigma > 0.f ? kTlWeightUnit / sigma : 0.f;
+                *reinterpret_cast<float4 *>(stage + lane * 16) = make_float4(sc.x * g, sc.y * g, sc.z * g, sc.w * g);
+                const int t_first = __shfl_sync(~0u, t, 0), t_last = __shfl_sync(~0u, t, 12);
+                const bool row = __all_sync(~0u, t != kTlHidden) && t_last - t_first == kTlKeys - 16;
+                if (keys && (lane & 3) == 0) *reinterpret_cast<int *>(stage + M::kFirst + lane) = t;
+                if (lane == 0) {
+                    *reinterpret_cast<int *>(stage + M::kFirst + 16) = row ? t_first : -1;
+                    *reinterpret_cast<float *>(stage + M::kFirst + 20) = turn;
+                    *reinterpret_cast<float *>(stage + M::kFirst + 24) = sigma;
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(kBarScales + (i & 3)));
+                fetch();
+                look_up(i + 2);
+                if (++st == kTlStages) { st = 0; phase ^= 1; }
+            }
+        } else if (qt < W.n_q && lane == 0 && W.n_tiles > 0) {
             const uint32_t s_at = W.tmem + qt * 2 * kTlKeys, o_at = W.tmem + 4 * kTlKeys + qt * D;
             const int n_tiles = W.n_tiles;
             const uint32_t idesc_s = umma_idesc_f16_m128(kTlKeys), idesc_o = umma_idesc_f16_m128(D) | 1u << 16;   // B: channels contiguous
@@ -639,33 +659,36 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                 if (!failed && !wait_phase(bar(b), parity)) failed = true;
                 return !failed;
             };
-            auto scores = [&](int i) {
-                if (!wait(kBarKFull + (i & (kTlStages - 1)), (i / kTlStages) & 1)) return;
+            int k_st = 0, k_turn = 0, v_st = 0;                     // stage and phase of the next scores, stage of the next values
+            auto scores = [&](int i) {                             // (the keys and values of a step become full together)
+                if (!wait(kBarFull + k_st, k_turn)) return;
                 tc_fence_after_sync();
-                const uint32_t k = k_lo + (i & (kTlStages - 1)) * (M::kKV1 >> 4), to = s_at + (i & 1) * kTlKeys;
+                const uint32_t k = k_lo + k_st * (M::kKV1 >> 4), to = s_at + (i & 1) * kTlKeys;
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)
                     mma_ss(to, q_lo + (ks >> 2) * (kTlRows * 128 >> 4) + (ks & 3) * 2, k + (ks >> 2) * (kTlKeys * 128 >> 4) + (ks & 3) * 2,
                            idesc_s, ks != 0);
                 umma_commit(bar(kBarS + qt * 2 + (i & 1)));
-                umma_commit(bar(kBarKFree + (i & (kTlStages - 1))));
+                umma_commit(bar(kBarKFree + k_st));
+                if (++k_st == kTlStages) { k_st = 0; k_turn ^= 1; }
             };
             // Scores run two steps ahead of the values: step i + 2's go where step i's weights were, after the contraction that
             // reads those (this thread issues both, and they execute in order).
             if (wait(kBarQ, 0))
                 for (int i = 0; i < 2 && i < n_tiles && !failed; ++i) scores(i);
+#pragma unroll 1
             for (int i = 0; i < n_tiles && !failed; ++i) {
-                const int st = i & (kTlStages - 1);
-                if (!wait(kBarVFull + st, (i / kTlStages) & 1) || !wait(kBarP + qt * 2 + (i & 1), (i >> 1) & 1)) break;
+                if (!wait(kBarP + qt * 2 + (i & 1), (i >> 1) & 1)) break;
                 tc_fence_after_sync();
-                const uint32_t v = v_lo + st * (M::kKV1 >> 4), p = s_at + (i & 1) * kTlKeys;
+                const uint32_t v = v_lo + v_st * (M::kKV1 >> 4), p = s_at + (i & 1) * kTlKeys;
 #pragma unroll
                 for (int ks = 0; ks < kTlKeys / 16; ++ks) {
                     mma_ts(o_at, p + weight_column(ks), v + ks * (2048 >> 4), idesc_o, ks != 0 || i != 0);
                     if (SPLIT) mma_ts(o_at, p + weight_column(ks) + 16, v + ks * (2048 >> 4), idesc_o, true);
                 }
                 umma_commit(bar(kBarPV + qt * 2 + (i & 1)));
-                umma_commit(bar(kBarVFree + st));
+                umma_commit(bar(kBarVFree + v_st));
+                if (++v_st == kTlStages) v_st = 0;
                 if (i + 2 < n_tiles) scores(i + 2);
             }
             umma_commit(bar(kBarO + qt));
