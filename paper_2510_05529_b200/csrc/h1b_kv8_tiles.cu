@@ -28,10 +28,11 @@ namespace h1b {
 namespace {
 
 constexpr int kTlRows = 128, kTlKeys = 64, kTlBlocks = kTlKeys / kKv8Block;
-constexpr int kTlThreads = 20 * 32;                            // warps 0-7 softmax, 8-15 convert, 16-17 issue, 18 scales;
-                                                                // 19 only hands over its registers
-constexpr int kTlRegsLaunch = 96, kTlRegsSoftmax = 152, kTlRegsConvert = 56, kTlRegsIssue = 64;
-static_assert(256 * kTlRegsSoftmax + 256 * kTlRegsConvert + 128 * kTlRegsIssue <= kTlThreads * kTlRegsLaunch,
+constexpr int kTlHalves = 1;                                   // 16-row fragments a softmax warp has
+constexpr int kTlSoftmax = 16 / kTlHalves;                     // warps 0 .. softmax, then 8 convert, 2 issue, 1 scales;
+constexpr int kTlThreads = (kTlSoftmax + 12) * 32;             // the last only hands over its registers
+constexpr int kTlRegsLaunch = kTlHalves == 1 ? 72 : 96, kTlRegsSoftmax = kTlHalves == 1 ? 88 : 152, kTlRegsConvert = 48, kTlRegsIssue = 56;
+static_assert(kTlSoftmax * 32 * kTlRegsSoftmax + 256 * kTlRegsConvert + 128 * kTlRegsIssue <= kTlThreads * kTlRegsLaunch,
               "more registers than a block is launched with");
 constexpr float kTlLazy = 4.f, kTlWeightUnit = 512.f;
 constexpr int kTlHidden = 1 << 30;                             // "first token" of a block that nobody sees: beyond every position
@@ -52,7 +53,8 @@ struct TlSmem {
     static constexpr int kQ1 = kTlRows * D * 2, kKV1 = kTlKeys * D * 2, kRaw1 = 2 * kTlKeys * D;
     static constexpr int kQ = 0, kK = 2 * kQ1, kV = kK + kTlStages * kKV1, kRaw = kV + kTlStages * kKV1;
     static constexpr int kScales = kRaw + kTlRawStages * kRaw1;
-    // per scale stage: ks [64], vs / sigma [64], blocks' first tokens [4], {first token if all 64 are in a row, else -1; turn; sigma}
+    // per scale stage: ks [64], vs / sigma [64], blocks' first tokens [4], {turn, sigma}, {for tiles A and B: bit 0 every row
+    // sees all 64 tokens, bit 1 turn is not 1}
     static constexpr int kVs = kTlKeys * 4, kFirst = 2 * kTlKeys * 4, kStage = kFirst + 32;
     static constexpr int kRows = kScales + kTlScaleStages * kStage;              // qs [256], positions [256]
     static constexpr int kBars = kRows + 2 * kTlRows * 8;
@@ -208,12 +210,13 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
     }
     __syncthreads();
     if (!W.go) return;
-    if (warp == 16) tmem_alloc(smem_addr(&work_s.tmem), 512);
+    if (warp == kTlSoftmax + 8) tmem_alloc(smem_addr(&work_s.tmem), 512);
     if (tid == 0) {
         for (int i = 0; i < kBarCount; ++i) {                    // arrivals: one a warp, or one commit
             int n = 1;
-            if (i == kBarQ || (i >= kBarFull && i < kBarKFree)) n = 8;
-            else if (i >= kBarP && i < kBarPV) n = 4;
+            if (i == kBarQ) n = kTlSoftmax;
+            else if (i >= kBarFull && i < kBarKFree) n = 8;
+            else if (i >= kBarP && i < kBarPV) n = kTlSoftmax / 2;
             else if (i >= kBarKFree && i < kBarScales) n = W.n_q;
             mbar_init(bar(i), n);
         }
@@ -224,16 +227,18 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
     tc_fence_after_sync();
     bool failed = false;
 
-    if (warp < 8) {
+    if (warp < kTlSoftmax) {
         more_registers<kTlRegsSoftmax>();
         // ---------------------------------------------------------------------------------------- softmax
         // A warp has 32 rows of a tile in fragment layout: rows gi + 8 q (q = 0 .. 3) of them are this lane's, four lanes to a
         // row. (A warp reaches the quarter of tensor memory of its number % 4.)
-        const int qt = warp >> 2, gi = lane >> 2, tj = lane & 3, row0 = (warp & 3) * 32;
+        const int qt = warp / (kTlSoftmax / 2), gi = lane >> 2, tj = lane & 3;
+        const int row0 = (warp & 3) * 32 + (kTlHalves == 1 ? (warp & 4) * 4 : 0);
+        constexpr int NQ = 2 * kTlHalves;
         // the query rows, two threads to a row: fp16 multiplied by 2^-e, negated if the scale is negative, into the K-major
         // operand
 #pragma unroll 1
-        for (int r = tid >> 1; r < 2 * kTlRows; r += 128) {
+        for (int r = tid >> 1; r < 2 * kTlRows; r += kTlSoftmax * 16) {
             const int half = tid & 1;
             const int pair = W.pair0 + r, tok = pair / A.group, head = (int)(blockIdx.x % P.hkv) * A.group + pair % A.group;
             const bool live = r < W.pairs;
@@ -278,13 +283,10 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
         if (!warp_wait(bar(kBarQ), 0)) failed = true;            // (the rows of a warp came through others)
 
         const uint32_t t_lane = W.tmem + ((uint32_t)row0 << 16), t_o = t_lane + 4 * kTlKeys + qt * D;
-        // the tile's smallest and largest position
-        const int qpos0 = W.seq_pos + (W.pair0 + qt * kTlRows) / A.group;
-        const int qpos1 = W.seq_pos + (W.pair0 + min(W.pairs, qt * kTlRows + kTlRows) - 1) / A.group;
         const int n_tiles = W.n_tiles;
-        uint64_t qs2[4], nm2[4], l2[4];                          // of each row, twice: qs, -m, and the two halves of the sum
+        uint64_t qs2[NQ], nm2[NQ], l2[NQ];                          // of each row, twice: qs, -m, and the two halves of the sum
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (int q = 0; q < NQ; ++q) {
             const float qs = reinterpret_cast<const float *>(smem + M::kRows)[qt * kTlRows + row0 + 8 * q + gi];
             qs2[q] = pack2f(qs, qs);
             nm2[q] = pack2f(INFINITY, INFINITY);
@@ -299,25 +301,24 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                 }
                 tc_fence_after_sync();
                 const uint32_t t_s = t_lane + (qt * 2 + (i & 1)) * kTlKeys;
-                uint32_t sv[2][2][16];                            // [32 columns][16 rows]
+                uint32_t sv[2][kTlHalves][16];                            // [32 columns][16 rows]
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) tmem_ld_frag_issue(t_s + c * 32 + ((uint32_t)(16 * h) << 16), sv[c][h]);
+                    for (int h = 0; h < kTlHalves; ++h) tmem_ld_frag_issue(t_s + c * 32 + ((uint32_t)(16 * h) << 16), sv[c][h]);
                 const unsigned char *stage = smem + M::kScales + (i & 3) * M::kStage;
                 const unsigned char *ks = stage + tj * 8, *vs = ks + M::kVs;   // pairs of columns 8 b + 2 tj, + 1
                 const int *first = reinterpret_cast<const int *>(stage + M::kFirst);
-                const int t0 = first[4];
-                const float turn = reinterpret_cast<const float *>(stage + M::kFirst)[5];
-                const bool whole = t0 >= 0 && t0 + kTlKeys - 1 <= qpos0 && (!A.window || t0 > qpos1 - A.window || t0 + kTlKeys - 1 < A.sinks);
+                const int how = first[6 + qt];
+                const bool whole = how & 1;
                 // bit 2 b + x of seen[q]: row q of the lane sees column 8 b + 2 tj + x
-                uint32_t seen[4] = {0, 0, 0, 0};
+                uint32_t seen[NQ] = {};
                 if (!whole) {
 #pragma unroll 1
                     for (int b = 7; b >= 0; --b) {
                         const int t = first[b >> 1] + (b & 1) * 8 + 2 * tj;
 #pragma unroll
-                        for (int q = 0; q < 4; ++q) {
+                        for (int q = 0; q < NQ; ++q) {
                             const int pos = row_pos[8 * q];
                             const bool s0 = t <= pos && (!A.window || t > pos - A.window || t < A.sinks);
                             const bool s1 = t + 1 <= pos && (!A.window || t + 1 > pos - A.window || t + 1 < A.sinks);
@@ -329,14 +330,16 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
 #pragma unroll
                 for (int c = 0; c < 2; ++c)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) tmem_tie16(sv[c][h]);
+                    for (int h = 0; h < kTlHalves; ++h) tmem_tie16(sv[c][h]);
                 // ---- scores times the keys' scales, and the rows' largest (before qs >= 0) ----
-                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                float top[NQ];
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) top[q] = -INFINITY;
 #pragma unroll
                 for (int b = 0; b < 8; ++b) {
                     const uint64_t kk = *reinterpret_cast<const uint64_t *>(ks + b * 32);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
+                    for (int q = 0; q < NQ; ++q) {
                         uint32_t *r = &sv[b >> 2][q >> 1][(b & 3) * 4 + (q & 1) * 2];
                         const float2 z = unpack2(mul2(pack2(r[0], r[1]), kk));
                         r[0] = __float_as_uint(z.x);
@@ -347,7 +350,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
 #pragma unroll
                     for (int b = 0; b < 8; ++b)
 #pragma unroll
-                        for (int q = 0; q < 4; ++q)
+                        for (int q = 0; q < NQ; ++q)
 #pragma unroll
                             for (int x = 0; x < 2; ++x)
                                 if (!(seen[q] >> (2 * b + x) & 1)) sv[b >> 2][q >> 1][(b & 3) * 4 + (q & 1) * 2 + x] = 0xFF800000u;
@@ -355,17 +358,18 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
 #pragma unroll
                 for (int b = 0; b < 8; ++b)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
+                    for (int q = 0; q < NQ; ++q) {
                         const uint32_t *r = &sv[b >> 2][q >> 1][(b & 3) * 4 + (q & 1) * 2];
                         top[q] = max3(top[q], __uint_as_float(r[0]), __uint_as_float(r[1]));
                     }
                 float over = -INFINITY;                           // how far a score lies above its row's reference
 #pragma unroll
-                for (int q = 0; q < 4; ++q) over = fmaxf(over, fmaf(top[q], unpack2(qs2[q]).x, unpack2(nm2[q]).x));
-                if (__any_sync(~0u, over > kTlLazy) || turn != 1.f) {
-                    float f[4];
+                for (int q = 0; q < NQ; ++q) over = fmaxf(over, fmaf(top[q], unpack2(qs2[q]).x, unpack2(nm2[q]).x));
+                if (__any_sync(~0u, over > kTlLazy) || (how & 2)) {
+                    const float turn = reinterpret_cast<const float *>(first)[4];
+                    float f[NQ];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
+                    for (int q = 0; q < NQ; ++q) {
                         const float m = -unpack2(nm2[q]).x;
                         float x = top[q] == -INFINITY ? top[q] : top[q] * unpack2(qs2[q]).x;
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
@@ -382,7 +386,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                         if (!warp_wait(bar(kBarPV + qt * 2 + ((i - 1) & 1)), ((i - 1) >> 1) & 1)) { failed = true; break; }
                         tc_fence_after_sync();
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
+                        for (int h = 0; h < kTlHalves; ++h)
 #pragma unroll 1
                             for (int c = 0; c < D; c += 32) {
                                 const uint32_t at = t_o + c + ((uint32_t)(16 * h) << 16);
@@ -402,12 +406,12 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                     constexpr bool MASK = decltype(masked)::value;
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        uint32_t hi[2][8], lo[2][8];
+                        uint32_t hi[kTlHalves][8], lo[kTlHalves][8];
 #pragma unroll
                         for (int b = 0; b < 4; ++b) {
                             const uint64_t vv = *reinterpret_cast<const uint64_t *>(vs + (c * 4 + b) * 32);
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) {
+                            for (int q = 0; q < NQ; ++q) {
                                 const uint32_t *r = &sv[c][q >> 1][b * 4 + (q & 1) * 2];
                                 const float2 z = unpack2(fma2(pack2(r[0], r[1]), qs2[q], nm2[q]));
                                 float p0 = ex2_approx(z.x), p1 = ex2_approx(z.y);
@@ -437,7 +441,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                             }
                         }
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
+                        for (int h = 0; h < kTlHalves; ++h) {
                             const uint32_t to = t_s + c * 32 + ((uint32_t)(16 * h) << 16);
                             if (SPLIT) tmem_st_frag32(to, hi[h], lo[h]);
                             else tmem_st_frag16(to, hi[h]);
@@ -455,14 +459,14 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
             tc_fence_after_sync();
             if (!failed) {
                 float sigma = 0.f;
-                if (n_tiles > 0) sigma = reinterpret_cast<const float *>(smem + M::kScales + ((n_tiles - 1) & 3) * M::kStage + M::kFirst)[6];
+                if (n_tiles > 0) sigma = reinterpret_cast<const float *>(smem + M::kScales + ((n_tiles - 1) & 3) * M::kStage + M::kFirst)[5];
                 const int parts = W.parts;
-                float inv[4];
-                bool live[4];
-                uint16_t *op[4];
-                float *pa[4];
+                float inv[NQ];
+                bool live[NQ];
+                uint16_t *op[NQ];
+                float *pa[NQ];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
+                for (int q = 0; q < NQ; ++q) {
                     const float2 x = unpack2(l2[q]);
                     float l = x.x + x.y;
                     l += __shfl_xor_sync(~0u, l, 1);
@@ -482,7 +486,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                     }
                 }
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < kTlHalves; ++h)
 #pragma unroll 1
                     for (int c = 0; c < D; c += 32) {
                         uint32_t ov[16];
@@ -506,10 +510,10 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                     }
             }
         }
-    } else if (warp < 16) {
+    } else if (warp < kTlSoftmax + 8) {
         fewer_registers<kTlRegsConvert>();
         // ---------------------------------------------------------------------------------------- convert
-        const bool keys = warp < 12;                                           // warps 8-11 keys, 12-15 values
+        const bool keys = warp < kTlSoftmax + 4;                                           // warps 8-11 keys, 12-15 values
         const int cw = warp & 3;
         constexpr int ROWS_IT = D == 128 ? 4 : 8, ITS = 16 / ROWS_IT;          // rows per 512 bytes, loads per thread and step
         // A warp converts one block of each step. lane -> (row, 16 channels) such that eight neighbouring lanes write 128
@@ -519,7 +523,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
         const int rr = D == 128 ? ((lane >> 2) & 1) | ((lane >> 4) & 1) << 1 : lane >> 2;
         const uint8_t *codes = (keys ? P.k : P.v) + (int64_t)(blockIdx.x % P.hkv) * P.page_tokens * D + rr * D + grp * 16;
         const int32_t *table = P.table + (int64_t)W.seq * P.table_width;
-        const uint32_t raw = sm + M::kRaw + (warp - 8) * 16 * D + lane * 16;
+        const uint32_t raw = sm + M::kRaw + (warp - kTlSoftmax) * 16 * D + lane * 16;
         const int n_tiles = W.n_tiles, j_first = W.j0 + cw, j1 = W.j1, sink_blocks = W.sink_blocks, skip = W.first - sink_blocks;
         int offset = 0, page = -1;                                              // asked for last: the block's place in its page, the page
         auto look_up = [&](int i) {
@@ -575,8 +579,8 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
         // ---------------------------------------------------------------------------------------- issue
         // A thread for each of the two tiles: a wait that need not wait still takes it some 200 cycles, and one thread for
         // both had no time left to keep the tensor cores busy.
-        const int qt = warp - 16;
-        if (warp == 18) {
+        const int qt = warp - (kTlSoftmax + 8);
+        if (qt == 2) {
             // ------------------------------------------------------------------------------------ scales
             // Lanes 4 x .. 4 x + 3 look after block x % 4 of a step: its first token, its page, and the scales of tokens
             // 4 (lane % 4) .. + 3 of it, the keys' (lanes 0 - 15) or the values' (16 - 31). The table is read two steps ahead,
@@ -586,6 +590,9 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
             const int32_t *table = P.table + (int64_t)W.seq * P.table_width;
             const int n_tiles = W.n_tiles, j_first = W.j0 + ((lane >> 2) & 3), j1 = W.j1, sink_blocks = W.sink_blocks, skip = W.first - sink_blocks;
             const int lo = W.lo, hi = W.hi, sinks = W.sinks;
+            // the smallest and largest position of tile A (lane 0) and B (lane 1)
+            const int pos0 = W.seq_pos + (W.pair0 + (lane & 1) * kTlRows) / A.group;
+            const int pos1 = W.seq_pos + (W.pair0 + min(W.pairs, (lane & 1) * kTlRows + kTlRows) - 1) / A.group;
             int t_next = kTlHidden, offset = 0, page = -1;
             auto look_up = [&](int i) {
                 const int j = j_first + i * kTlBlocks;
@@ -638,10 +645,10 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                 const int t_first = __shfl_sync(~0u, t, 0), t_last = __shfl_sync(~0u, t, 12);
                 const bool row = __all_sync(~0u, t != kTlHidden) && t_last - t_first == kTlKeys - 16;
                 if (keys && (lane & 3) == 0) *reinterpret_cast<int *>(stage + M::kFirst + lane) = t;
-                if (lane == 0) {
-                    *reinterpret_cast<int *>(stage + M::kFirst + 16) = row ? t_first : -1;
-                    *reinterpret_cast<float *>(stage + M::kFirst + 20) = turn;
-                    *reinterpret_cast<float *>(stage + M::kFirst + 24) = sigma;
+                if (lane < 2) {                                                 // a lane for each tile
+                    const bool whole = row && t_last + 15 <= pos0 && (!A.window || t_first > pos1 - A.window || t_last + 15 < A.sinks);
+                    reinterpret_cast<int *>(stage + M::kFirst)[6 + lane] = (int)whole | (turn != 1.f ? 2 : 0);
+                    reinterpret_cast<float *>(stage + M::kFirst)[4 + lane] = lane ? sigma : turn;
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar(kBarScales + (i & 3)));
@@ -699,7 +706,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
     __syncwarp();
     tc_fence_before_sync();
     __syncthreads();
-    if (warp == 16) { tc_fence_after_sync(); tmem_dealloc(W.tmem, 512); }
+    if (warp == kTlSoftmax + 8) { tc_fence_after_sync(); tmem_dealloc(W.tmem, 512); }
 }
 
 template <int D, int FMT, bool SPLIT>
