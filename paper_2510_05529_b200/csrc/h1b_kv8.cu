@@ -22,7 +22,7 @@ __device__ __forceinline__ int64_t kv8_place(const Kv8Params &P, const Kv8Seq &s
     const int pos = s.kv - s.n + (r - s.start);
     if (pos < 0) { kv8_report(P, H1B_ERR_INVALID_ARG); return -1; }
     if (pos >= P.cap) { kv8_report(P, H1B_ERR_CAPACITY); return -1; }
-    const int col = pos / P.page_tokens, page = P.table[(int64_t)s.b * P.table_width + col];
+    const int col = kv8_page_of(P, pos / kKv8Block), page = P.table[(int64_t)s.b * P.table_width + col];
     if (page < 0 || page >= P.n_pages) { kv8_report(P, H1B_ERR_BOUNDS); return -1; }
     return (int64_t)page * P.hkv * P.page_tokens + (pos - col * P.page_tokens);
 }
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Io io, const int
         if (at >= 0) {
             const int64_t row = at + (int64_t)h * P.page_tokens;
             const uint2 c = *reinterpret_cast<const uint2 *>(((x & 1) ? P.v : P.k) + row * D + sub * 8);
-            const float sc = ((x & 1) ? P.vs : P.ks)[row] * kv8_unit<FMT>();   // (a power of two: exact)
+            const float sc = ((x & 1) ? P.vs : P.ks)[row];
             uint32_t hh[4];
             kv8_codes4<FMT>(c.x, hh[0], hh[1]);
             kv8_codes4<FMT>(c.y, hh[2], hh[3]);
@@ -171,7 +171,7 @@ cudaError_t launch_io(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_r
 // (2^-12 on average) vanishes beside that of a bf16 result, but would add as much again to an fp16 result's: there (SPLIT)
 // a second product carries what the rounding left, w = hi + lo to 2^-22, at no cost in time where the loads are the bound.
 // ------------------------------------------------------------------------------------------------------------------
-constexpr int kRowsStages = 4;
+constexpr int kRowsStages = 3;
 constexpr int kRowsWarps = 4;
 constexpr float kLazy = 2.f;
 constexpr float kWeightUnit = 2048.f;
@@ -183,7 +183,7 @@ __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
 }
 
 template <int D>
-__host__ __device__ constexpr int rows_stage_bytes() { return 32 * D + 128 + 16; }
+__host__ __device__ constexpr int rows_stage_bytes() { return 32 * D + 128; }
 template <int D, int NB>
 __host__ __device__ constexpr int rows_smem_bytes() {
     const int ring = kRowsWarps * kRowsStages * rows_stage_bytes<D>(), merge = kRowsWarps * 8 * NB * (D + 2) * 4;
@@ -191,7 +191,7 @@ __host__ __device__ constexpr int rows_smem_bytes() {
 }
 
 template <int D, int FMT, int NB, bool SPLIT>
-__global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_kernel(const Kv8Params P, const Kv8Attn A) {
+__global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_kernel(const Kv8Params P, const Kv8Attn A) {
     extern __shared__ __align__(128) unsigned char smem[];
     constexpr int R = 8 * NB, STAGE = rows_stage_bytes<D>();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -215,44 +215,44 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_ker
         const int j0 = split * per, j1 = min(j0 + per, span.count);
         const int n_mine = j1 - j0 > warp ? (j1 - j0 - warp + kRowsWarps - 1) / kRowsWarps : 0;
 
-        // ---- the copies: block i of this warp into stage i % kRowsStages; page numbers come 32 blocks at a time ----
+        // ---- the copies: block i of this warp into stage i % 3; where the blocks lie is looked up 32 blocks at a time ----
         const int32_t *table = P.table + (int64_t)s.b * P.table_width;
-        int page_lane = -1;
-        auto issue = [&](int i) {
+        const uint8_t *kp = P.k + lane * 16, *vp = P.v + lane * 16;
+        const float *sp = (lane < 4 ? P.ks : P.vs) + (lane & 3) * 4;
+        int at_lane = -1;                                        // block i + lane of the warp: its number in the pool, or -1
+        auto issue = [&](int i, int stage) -> int {              // -> the block's first token, or -1: nobody sees it
+            int t = -1;
             if (i < n_mine) {
                 if ((i & 31) == 0) {
-                    const int j = j0 + warp + (i + lane) * kRowsWarps;
-                    page_lane = i + lane < n_mine ? table[span.token(j) / P.page_tokens] : -1;
-                    if (i + lane < n_mine && (page_lane < 0 || page_lane >= P.n_pages)) {
-                        kv8_report(P, H1B_ERR_BOUNDS);
-                        page_lane = -1;
+                    at_lane = -1;
+                    if (i + lane < n_mine) {
+                        const int blk = span.token(j0 + warp + (i + lane) * kRowsWarps) / kKv8Block, col = kv8_page_of(P, blk);
+                        const int page = table[col], per_page = P.page_tokens / kKv8Block;
+                        if (page >= 0 && page < P.n_pages) at_lane = (page * P.hkv + kvh) * per_page + blk - col * per_page;
+                        else kv8_report(P, H1B_ERR_BOUNDS);
                     }
                 }
-                const int page = __shfl_sync(~0u, page_lane, i & 31);
-                const int t = span.token(j0 + warp + i * kRowsWarps);
-                const uint32_t st = ring + (i % kRowsStages) * STAGE;
-                if (page >= 0) {
-                    const int64_t at = ((int64_t)page * P.hkv + kvh) * P.page_tokens + t % P.page_tokens;
-                    const uint8_t *kp = P.k + at * D, *vp = P.v + at * D;
+                const int at = __shfl_sync(~0u, at_lane, i & 31);
+                if (at >= 0) {
+                    t = span.token(j0 + warp + i * kRowsWarps);
+                    const uint32_t st = ring + stage * STAGE;
+                    const uint8_t *ks = kp + (int64_t)at * (16 * D), *vs = vp + (int64_t)at * (16 * D);
 #pragma unroll
                     for (int c = 0; c < D / 32; ++c) {
                         const int x = lane + 32 * c, r = x / (D / 16), ch = x % (D / 16);
                         const uint32_t kd = D == 128 ? r * 128 + ((ch ^ ((r & 1) << 2)) << 4) : x << 4;
                         const uint32_t vd = D == 128 ? r * 128 + ((ch ^ (r & 7)) << 4)
                                                      : (r >> 1) * 128 + (((((r & 1) << 2) | ch) ^ (((r >> 1) & 3) << 1)) << 4);
-                        cp_async_16(st + kd, kp + x * 16, 16);
-                        cp_async_16(st + 16 * D + vd, vp + x * 16, 16);
+                        cp_async_16(st + kd, ks + c * 512, 16);
+                        cp_async_16(st + 16 * D + vd, vs + c * 512, 16);
                     }
-                    if (lane < 8)
-                        cp_async_16(st + 32 * D + lane * 16, (lane < 4 ? P.ks : P.vs) + at + (lane & 3) * 4, 16);
+                    if (lane < 8) cp_async_16(st + 32 * D + lane * 16, sp + (int64_t)at * kKv8Block, 16);
                 }
-                if (lane == 0)                                   // the block's first token, or -1: nobody sees it
-                    *reinterpret_cast<int *>(smem + (st - smem_addr(smem)) + 32 * D + 128) = page >= 0 ? t : -1;
             }
             cp_async_commit();
+            return t;
         };
-#pragma unroll
-        for (int i = 0; i < kRowsStages - 1; ++i) issue(i);
+        int t_now = issue(0, 0), t_next = issue(1, 1);
 
         // ---- the query rows, as B operands: lane (n = gi, k pair tj) holds channels 16 (tj + 4 c) .. + 15 of row gi ----
         uint32_t qf[NB][D / 16][2];
@@ -285,12 +285,12 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_ker
             amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
             amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
             const int e = kv8_row_exponent(amax);
-            const float up = pow2i(-e);
+            const float up = A.scale_log2 < 0.f ? -pow2i(-e) : pow2i(-e);   // (so that qs >= 0)
 #pragma unroll
             for (int i = 0; i < D / 16; ++i)
 #pragma unroll
                 for (int y = 0; y < 2; ++y) qf[nb][i][y] = pack_f16x2(f[i][y].x * up, f[i][y].y * up);
-            const float unit = A.scale_log2 * kv8_unit<FMT>() * pow2i(e);
+            const float unit = fabsf(A.scale_log2) * pow2i(e);
             const int t0 = s.kv - s.n + tok;
 #pragma unroll
             for (int y = 0; y < 2; ++y) {
@@ -299,22 +299,25 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_ker
             }
         }
 
-        float o[NB][D / 16][4], m[NB][2], l[NB][2];
+        float o[NB][D / 16][4], nm[NB][2], l[NB][2];             // nm: -m
         float sigma = 0.f, wscale = 0.f;                         // wscale = kWeightUnit / sigma
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) o[nb][i][0] = o[nb][i][1] = o[nb][i][2] = o[nb][i][3] = 0.f;
-            m[nb][0] = m[nb][1] = -INFINITY;
+            nm[nb][0] = nm[nb][1] = INFINITY;
             l[nb][0] = l[nb][1] = 0.f;
         }
 
+        int stage = 0;
         for (int i = 0; i < n_mine; ++i) {
             cp_async_wait_group<kRowsStages - 2>();
             __syncwarp();                                        // every lane's copies of block i are there; block i - 1 is read
-            issue(i + kRowsStages - 1);
-            const unsigned char *st = smem + warp * kRowsStages * STAGE + (i % kRowsStages) * STAGE;
-            const int t = *reinterpret_cast<const int *>(st + 32 * D + 128);
+            const int t = t_now;
+            const unsigned char *st = smem + (warp * kRowsStages + stage) * STAGE;
+            t_now = t_next;
+            t_next = issue(i + 2, stage == 0 ? 2 : stage - 1);
+            stage = stage == 2 ? 0 : stage + 1;
             if (t < 0) continue;
             // ---- scores ----
             float c[NB][4];
@@ -339,32 +342,40 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_ker
             const float *sc = reinterpret_cast<const float *>(st + 32 * D);
             const float ks0 = sc[gi], ks1 = sc[gi + 8];
             float vs0 = sc[16 + gi], vs1 = sc[16 + gi + 8];
-            const int t0 = t + gi, t1 = t0 + 8;
             // all rows of the tile see all 16 tokens, or each pair is looked at
             const bool whole = t + 15 <= pos0 && (!A.window || t > pos1 - A.window || t + 15 < A.sinks);
-            bool see[NB][4];
-            float big = 0.f;
+            uint32_t hidden = 0;                                 // bit 4 nb + y: token gi (+ 8 for y >= 2) is not seen by row 2 tj + y % 2
+            float over = -INFINITY;                              // how far a score lies above its row's reference
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    const int tt = (y & 2) ? t1 : t0, p = pos[nb][y & 1];
-                    see[nb][y] = whole || (tt <= p && (!A.window || tt > p - A.window || tt < A.sinks));
-                    c[nb][y] = see[nb][y] ? c[nb][y] * ((y & 2) ? ks1 : ks0) * qs[nb][y & 1] : -INFINITY;
-                    big = fmaxf(big, c[nb][y] - m[nb][y & 1] > kLazy ? 1.f : 0.f);
-                }
-            if (!whole) {                                        // scales of tokens that no row sees say nothing
+                for (int y = 0; y < 4; ++y) c[nb][y] *= (y & 2) ? ks1 : ks0;
+            if (!whole) {
+                const int t0 = t + gi, t1 = t0 + 8;
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const int tt = (y & 2) ? t1 : t0, p = pos[nb][y & 1];
+                        if (tt <= p && (!A.window || tt > p - A.window || tt < A.sinks)) continue;
+                        hidden |= 1u << (4 * nb + y);
+                        c[nb][y] = -INFINITY;
+                    }
+                // scales of tokens that no row sees say nothing
                 if (!(t0 <= span.hi && (t0 >= span.lo || t0 < span.sinks))) vs0 = 0.f;
                 if (!(t1 <= span.hi && (t1 >= span.lo || t1 < span.sinks))) vs1 = 0.f;
             }
-            const float vbig = fmaxf(vs0 <= 3.402823466e38f ? vs0 : 0.f, vs1 <= 3.402823466e38f ? vs1 : 0.f);
-            if (__any_sync(~0u, big > 0.f || vbig > 4.f * sigma)) {
-                float mx = vbig;
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int y = 0; y < 2; ++y) over = fmaxf(over, fmaf(fmaxf(c[nb][y], c[nb][y + 2]), qs[nb][y], nm[nb][y]));
+            if (__any_sync(~0u, over > kLazy || fmaxf(vs0, vs1) > 4.f * sigma)) {
+                float mx = fmaxf(vs0 <= 3.402823466e38f ? vs0 : 0.f, vs1 <= 3.402823466e38f ? vs1 : 0.f);
 #pragma unroll
                 for (int x = 1; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, x));
                 float turn = 1.f;                                // old sigma / new sigma
                 if (mx > 4.f * sigma) {
-                    const int e = clampi((int)(__float_as_uint(mx) >> 23) - 126, -120, 126);   // 2^e > mx
+                    const int e = clampi((int)(__float_as_uint(mx) >> 23) - 126, -115, 126);   // 2^e > mx
                     const float next = pow2i(e);
                     turn = sigma / next;
                     sigma = next;
@@ -378,9 +389,11 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_ker
                         top = fmaxf(top, __shfl_xor_sync(~0u, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(~0u, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(~0u, top, 16));
-                        const float next = fmaxf(m[nb][y], top);
-                        const float f = next > m[nb][y] ? ex2_approx(m[nb][y] - next) : 1.f;   // (from -inf: 0)
-                        m[nb][y] = next;
+                        if (top != -INFINITY) top *= qs[nb][y];
+                        const float m = -nm[nb][y];
+                        const bool up = top > m;
+                        const float f = up ? ex2_approx(m - top) : 1.f;   // (from -inf: 0)
+                        if (up) nm[nb][y] = -top;
                         l[nb][y] *= f;
 #pragma unroll
                         for (int x = 0; x < D / 16; ++x) { o[nb][x][y] *= f * turn; o[nb][x][y + 2] *= f * turn; }
@@ -393,11 +406,21 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_ker
             for (int nb = 0; nb < NB; ++nb) {
                 float p[4];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) p[y] = see[nb][y] ? ex2_approx(c[nb][y] - m[nb][y & 1]) : 0.f;
+                for (int y = 0; y < 4; ++y) p[y] = ex2_approx(fmaf(c[nb][y], qs[nb][y & 1], nm[nb][y & 1]));
+                if (!whole) {
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        if (hidden >> (4 * nb + y) & 1) p[y] = 0.f;
+                }
                 l[nb][0] += p[0] + p[2];
                 l[nb][1] += p[1] + p[3];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) p[y] = see[nb][y] ? p[y] * ((y & 2) ? g1 : g0) : 0.f;
+                for (int y = 0; y < 4; ++y) p[y] *= (y & 2) ? g1 : g0;
+                if (!whole) {
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        if (hidden >> (4 * nb + y) & 1) p[y] = 0.f;
+                }
 #pragma unroll
                 for (int y = 0; y < 2; ++y) {
                     const uint32_t hi = pack_f16x2(p[2 * y], p[2 * y + 1]);
@@ -423,6 +446,15 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_ker
                     w[y][0] = u.x; w[y][1] = u.y;
                 }
             }
+            if (!whole) {                                        // codes that no row sees may be NaN patterns: zero times NaN is none
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    const int tt = t + 2 * tj + (y & 1) + (y & 2) * 4;
+                    if (tt <= span.hi && (tt >= span.lo || tt < span.sinks)) continue;
+#pragma unroll
+                    for (int x = 0; x < D / 32; ++x) w[y][x] = 0;
+                }
+            }
 #pragma unroll
             for (int x = 0; x < D / 32; ++x) {
                 uint32_t lo[4], hi[4];
@@ -444,7 +476,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_ker
         // ---- the four warps' results meet in shared memory: [warp][row][d], then m and l [warp][row] ----
         __syncthreads();
         float *acc = reinterpret_cast<float *>(smem), *ml = acc + kRowsWarps * R * D;
-        const float unit = sigma * (kv8_unit<FMT>() / kWeightUnit);
+        const float unit = sigma * (1.f / kWeightUnit);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
@@ -461,7 +493,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 3 : 2) kv8_rows_ker
                     a[2 * x + 1] = o[nb][x][y + 2] * unit;
                 }
                 // (a row whose every score is NaN has no maximum, and is not an empty row)
-                if (gi == 0) { ml[(warp * R + row) * 2] = sum != sum ? sum : m[nb][y]; ml[(warp * R + row) * 2 + 1] = sum; }
+                if (gi == 0) { ml[(warp * R + row) * 2] = sum != sum ? sum : -nm[nb][y]; ml[(warp * R + row) * 2 + 1] = sum; }
             }
         __syncthreads();
         constexpr int PER = D / 2;                               // channel pairs of a row

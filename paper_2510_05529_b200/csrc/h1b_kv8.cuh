@@ -139,19 +139,18 @@ __device__ __forceinline__ Kv8Span kv8_span(const Kv8Params &P, const Kv8Attn &A
     return s;
 }
 
-// Four 8-bit codes -> two fp16 pairs, exactly: int8 as it is (1024 + 128 + code assembled in the mantissa, minus 1152),
-// e4m3 times 2^-8 (the seven magnitude bits moved to the top of fp16's exponent and mantissa; its subnormals become
-// fp16's). A NaN pattern, which no row that was appended holds, becomes a finite number.
-constexpr float kE4m3Unit = 256.f;
-template <int FMT>
-__device__ __forceinline__ float kv8_unit() { return FMT == H1B_KV8_INT8 ? 1.f : kE4m3Unit; }
+// Four 8-bit codes -> two fp16 pairs, exactly. int8: 1024 + 128 + code assembled in the mantissa, minus 1152 (five
+// instructions); e4m3: the conversion instruction, which takes a pair from the lower half of a register (three). A NaN
+// pattern of e4m3, which no row that was appended holds, stays one.
 __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-__device__ __forceinline__ uint32_t e4m3_bits_to_f16x2(uint32_t t) {   // codes in the upper byte of each half
-    return (t & 0x80008000u) | ((t >> 1) & 0x3F803F80u);
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t w) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)w));
+    return r;
 }
 template <int FMT>
 __device__ __forceinline__ void kv8_codes4(uint32_t w, uint32_t &h01, uint32_t &h23) {
@@ -160,22 +159,15 @@ __device__ __forceinline__ void kv8_codes4(uint32_t w, uint32_t &h01, uint32_t &
         h01 = sub_f16x2(__byte_perm(w, 0x64646464u, 0x4140), 0x64806480u);
         h23 = sub_f16x2(__byte_perm(w, 0x64646464u, 0x4342), 0x64806480u);
     } else {
-        h01 = e4m3_bits_to_f16x2(__byte_perm(w, 0u, 0x1404));
-        h23 = e4m3_bits_to_f16x2(__byte_perm(w, 0u, 0x3424));
+        h01 = e4m3x2_to_f16x2(w);
+        h23 = e4m3x2_to_f16x2(w >> 16);
     }
 }
 // Codes of the same four channels of two tokens a, b -> pairs (a_i, b_i), i = 0 .. 3.
 template <int FMT>
 __device__ __forceinline__ void kv8_codes4x2(uint32_t a, uint32_t b, uint32_t (&h)[4]) {
-    if (FMT == H1B_KV8_INT8) {
-        kv8_codes4<FMT>(__byte_perm(a, b, 0x5140), h[0], h[1]);
-        kv8_codes4<FMT>(__byte_perm(a, b, 0x7362), h[2], h[3]);
-    } else {
-        h[0] = e4m3_bits_to_f16x2(__byte_perm(a, b, 0x4000));
-        h[1] = e4m3_bits_to_f16x2(__byte_perm(a, b, 0x5010));
-        h[2] = e4m3_bits_to_f16x2(__byte_perm(a, b, 0x6020));
-        h[3] = e4m3_bits_to_f16x2(__byte_perm(a, b, 0x7030));
-    }
+    kv8_codes4<FMT>(__byte_perm(a, b, 0x5140), h[0], h[1]);
+    kv8_codes4<FMT>(__byte_perm(a, b, 0x7362), h[2], h[3]);
 }
 
 __device__ __forceinline__ float2 pair_to_float2(uint32_t w, int bf16) {

@@ -35,6 +35,9 @@ int check_pool(const h1b_kv8_pool *p) {
                             p->n_kv_heads, p->device);
     if (p->page_tokens < kKv8Block || p->page_tokens % kKv8Block)
         return report_error(H1B_ERR_INVALID_ARG, "page_tokens = %d: a multiple of %d", p->page_tokens, kKv8Block);
+    if ((int64_t)p->n_pages * p->n_kv_heads > (int64_t)(1u << 31) / (p->page_tokens / kKv8Block) - 1)
+        return report_error(H1B_ERR_UNSUPPORTED, "%d pages of %d tokens of %d heads: 2^35 or more rows", p->n_pages, p->page_tokens,
+                            p->n_kv_heads);
     if (!p->k || !p->v || !p->k_scale || !p->v_scale) return report_error(H1B_ERR_NULL, "a pool pointer is NULL");
     if (!aligned16(p->k) || !aligned16(p->v) || !aligned16(p->k_scale) || !aligned16(p->v_scale))
         return report_error(H1B_ERR_INVALID_ARG, "a pool pointer is not 16-byte aligned");

@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                     make_uint4(h[0], h[1], h[2], h[3]);
             }
             if (half == 0) {
-                reinterpret_cast<float *>(smem + M::kRows)[r] = fabsf(A.scale_log2) * kv8_unit<FMT>() * pow2i(e);
+                reinterpret_cast<float *>(smem + M::kRows)[r] = fabsf(A.scale_log2) * pow2i(e);
                 reinterpret_cast<int *>(smem + M::kRows)[2 * kTlRows + r] = W.seq_pos + tok;
             }
         }
@@ -472,7 +472,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                     l += __shfl_xor_sync(~0u, l, 1);
                     l += __shfl_xor_sync(~0u, l, 2);
                     const bool empty = l == 0.f;
-                    inv[q] = empty ? 0.f : 1.f / l * (kv8_unit<FMT>() / kTlWeightUnit) * sigma;
+                    inv[q] = empty ? 0.f : 1.f / l * (1.f / kTlWeightUnit) * sigma;
                     const float lse2 = empty ? -INFINITY : log2f(l) - unpack2(nm2[q]).x;
                     const int r = qt * kTlRows + row0 + 8 * q + gi, pair = W.pair0 + r, tok = W.start + pair / A.group;
                     const int head = (int)(blockIdx.x % P.hkv) * A.group + pair % A.group;
@@ -525,12 +525,13 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
         const int32_t *table = P.table + (int64_t)W.seq * P.table_width;
         const uint32_t raw = sm + M::kRaw + (warp - kTlSoftmax) * 16 * D + lane * 16;
         const int n_tiles = W.n_tiles, j_first = W.j0 + cw, j1 = W.j1, sink_blocks = W.sink_blocks, skip = W.first - sink_blocks;
+        const int lo = W.lo, hi = W.hi, sinks = W.sinks;
         int offset = 0, page = -1;                                              // asked for last: the block's place in its page, the page
+        auto block_of = [&](int i) { const int j = j_first + i * kTlBlocks; return j < sink_blocks ? j : j + skip; };
         auto look_up = [&](int i) {
-            const int j = j_first + i * kTlBlocks;
             page = -1;
-            if (j >= j1) return;
-            const int blk = j < sink_blocks ? j : j + skip, col = kv8_page_of(P, blk);
+            if (j_first + i * kTlBlocks >= j1) return;
+            const int blk = block_of(i), col = kv8_page_of(P, blk);
             offset = blk * kKv8Block - col * P.page_tokens;
             page = table[col];
         };
@@ -555,7 +556,19 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
             if (i >= kTlStages && !warp_wait(bar((keys ? kBarKFree : kBarVFree) + st), phase)) { failed = true; break; }
             cp_async_wait_group<2>();                                           // this step's copies
             unsigned char *line = smem + (keys ? M::kK : M::kV) + st * M::kKV1 + (grp >> 2) * (kTlKeys * 128) + (16 * cw + rr) * 128;
-            const unsigned char *src = smem + (raw - sm) + st * M::kRaw1;
+            unsigned char *src = smem + (raw - sm) + st * M::kRaw1;
+            if (FMT == H1B_KV8_E4M3 && !keys) {
+                // codes that no row sees may be NaN patterns, and their weight zero times NaN is none: they become zeros (a key's
+                // only reach a score that is hidden)
+                const int t = block_of(i) * kKv8Block;
+                if (!(t + 15 <= hi && (t >= lo || t + 15 < sinks))) {
+#pragma unroll 1
+                    for (int it = 0; it < ITS; ++it) {
+                        const int tt = t + it * ROWS_IT + rr;
+                        if (!(tt <= hi && (tt >= lo || tt < sinks))) *reinterpret_cast<uint4 *>(src + it * 512) = make_uint4(0, 0, 0, 0);
+                    }
+                }
+            }
 #pragma unroll
             for (int it = 0; it < ITS; ++it) {
                 const int rw = it * ROWS_IT + rr, c0 = (grp & 3) * 2;          // (row % 8: the block's first row is a multiple of 16)
