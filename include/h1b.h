@@ -484,8 +484,8 @@ typedef struct {             /* one layer's pages; all pointers DEVICE          
  * sequence: rows [row_start[b], row_start[b + 1]) belong to sequence b and are
  * its last n_b = row_start[b + 1] - row_start[b] cached tokens; row r is the
  * token at position kv_len[b] - row_start[b + 1] + r. n_b may be 0. Rows from
- * row_start[n_seqs] on (and before row_start[0]) belong to nobody: they are not
- * read, and outputs keep what they held there. Token t of sequence b lives in
+ * row_start[n_seqs] on (and before row_start[0]) belong to nobody: what they hold
+ * has no effect, and outputs keep what they held there. Token t of sequence b lives in
  * page block_table[b][t / page_tokens]; entries whose tokens no row sees are
  * not read (pages that a window has left behind may be given away).
  * The lengths and tables are read by the kernels, so a replayed graph works on

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 import torch
@@ -457,16 +458,21 @@ def _int32(what: str, x) -> int:
     return int(x)
 
 
-def _kv8_rows(t: torch.Tensor, what: str, heads: int, d: int, dtype, device) -> h1b_kv8_rows:
-    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype:
-        raise TypeError("%s must be a tensor of dtype %s on %s" % (what, dtype, device))
+def _kv8_rows(t: torch.Tensor, what: str, heads: int, d: int, dtype, index: int) -> bytes:
+    """The h1b_kv8_rows of a tensor [n_rows, heads, d] on CUDA device `index`, as its bytes (ctypes takes them for a pointer)."""
+    if t.dtype is not dtype or t.get_device() != index:
+        raise TypeError("%s must be a tensor of dtype %s on cuda:%d" % (what, dtype, index))
     shape = t.shape
     if len(shape) != 3 or shape[1] != heads or shape[2] != d:
         raise ValueError("%s must be [n_rows, %d, %d], got %s" % (what, heads, d, tuple(shape)))
     row, head, last = t.stride()
     if last != 1:
         raise ValueError("the channels of %s must be contiguous" % what)
-    return h1b_kv8_rows(t.data_ptr(), row, head)
+    return _ROWS(t.data_ptr(), row, head)
+
+
+_ROWS = struct.Struct("=Qqq").pack                                                                      # h1b_kv8_rows
+_BATCH = struct.Struct("=QQQQiii4x").pack                                                              # h1b_kv8_batch
 
 
 class KV8Pages:
@@ -498,70 +504,71 @@ class KV8Pages:
         self._pool = h1b_kv8_pool(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n_pages,
                                   self.n_kv_heads, page_tokens, self.head_dim, _KV8_FORMATS[k_pages.dtype],
                                   self.device.index)
-        self._pool_ref = ctypes.byref(self._pool)
+        self._pool_at = ctypes.addressof(self._pool)
+        self._index = self.device.index
+        self._workspaces = {}                            # sizes of a call -> bytes (h1b_kv8_attention_bytes depends on nothing else)
 
     def _check(self, rc: int):
         if rc != H1B_OK:
             raise H1BError(rc, (self.lib.h1b_last_error(None) or b"").decode())
 
-    def _stream(self, stream):
-        return torch.cuda.current_stream(self.device) if stream is None else stream
+    def _stream(self, stream) -> int:
+        # (the raw handle of the current stream: making a Stream object takes longer than the kernel of a small call)
+        return torch._C._cuda_getCurrentRawStream(self._index) if stream is None else stream.cuda_stream
 
     def _empty(self, shape, dtype, stream):
         """A new tensor for use on `stream`: memory that another stream's pending work may still use is not handed out."""
-        if stream == torch.cuda.current_stream(self.device):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+        if stream is None:
+            return self.status.new_empty(shape, dtype=dtype)
         with torch.cuda.stream(stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
-    def _batch(self, block_table, kv_len, row_start, n_rows: int) -> h1b_kv8_batch:
-        device, i32 = self.device, torch.int32
-        for name, t in (("block_table", block_table), ("kv_len", kv_len), ("row_start", row_start)):
-            if not isinstance(t, torch.Tensor) or t.dtype != i32 or t.device != device or not t.is_contiguous():
-                raise TypeError("%s must be a contiguous int32 tensor on %s" % (name, device))
+    def _batch(self, block_table, kv_len, row_start, n_rows: int) -> bytes:
+        index, i32 = self._index, torch.int32
+        for t in (block_table, kv_len, row_start):
+            if t.dtype is not i32 or t.get_device() != index or not t.is_contiguous():
+                raise TypeError("block_table, kv_len and row_start must be contiguous int32 tensors on cuda:%d" % index)
         shape = block_table.shape
         if len(shape) != 2 or kv_len.shape != shape[:1] or row_start.dim() != 1 or row_start.shape[0] != shape[0] + 1:
             raise ValueError("block_table must be [B, W], kv_len [B], row_start [B + 1]")
-        return h1b_kv8_batch(block_table.data_ptr(), kv_len.data_ptr(), row_start.data_ptr(), self._status, shape[0],
-                             shape[1], n_rows)
+        return _BATCH(block_table.data_ptr(), kv_len.data_ptr(), row_start.data_ptr(), self._status, shape[0], shape[1], n_rows)
 
     def h1b_kv8_append(self, k: torch.Tensor, v: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor,
                        row_start: torch.Tensor, stream=None):
         """k, v: fp16 or bf16 CUDA [n_rows, Hkv, d] (rows and heads may be strided): quantised into their places."""
-        if k.dtype not in _KV8_TYPES:
+        kind = _KV8_TYPES.get(k.dtype)
+        if kind is None:
             raise TypeError("k must be float16 or bfloat16, got %s" % k.dtype)
         if k.shape != v.shape:
             raise ValueError("k and v must have the same shape")
-        kr = _kv8_rows(k, "k", self.n_kv_heads, self.head_dim, k.dtype, self.device)
-        vr = _kv8_rows(v, "v", self.n_kv_heads, self.head_dim, k.dtype, self.device)
+        kr = _kv8_rows(k, "k", self.n_kv_heads, self.head_dim, k.dtype, self._index)
+        vr = _kv8_rows(v, "v", self.n_kv_heads, self.head_dim, k.dtype, self._index)
         batch = self._batch(block_table, kv_len, row_start, k.shape[0])
-        self._check(self.lib.h1b_kv8_append(self._pool_ref, ctypes.byref(batch), ctypes.byref(kr), ctypes.byref(vr),
-                                            _KV8_TYPES[k.dtype], self._stream(stream).cuda_stream))
+        self._check(self.lib.h1b_kv8_append(self._pool_at, batch, kr, vr, kind, self._stream(stream)))
 
     def h1b_kv8_read(self, block_table: torch.Tensor, kv_len: torch.Tensor, row_start: torch.Tensor, n_rows: int | None = None,
                      dtype=torch.float16, k: torch.Tensor | None = None, v: torch.Tensor | None = None, stream=None):
         """Rows row_start[b] .. of every sequence read back -> (k, v) of `dtype` [n_rows, Hkv, d]. Given k and / or v, those are
         filled (and only those); else two new tensors of n_rows rows."""
-        stream = self._stream(stream)
         if k is None and v is None:
             if n_rows is None:
                 raise ValueError("n_rows, k or v must be given")
             if dtype not in _KV8_TYPES:
                 raise TypeError("dtype must be float16 or bfloat16, got %s" % dtype)
-            k, v = (self._empty((n_rows, self.n_kv_heads, self.head_dim), dtype, stream) for _ in "kv")
+            shape = (n_rows, self.n_kv_heads, self.head_dim)
+            k, v = self._empty(shape, dtype, stream), self._empty(shape, dtype, stream)
         given = k if k is not None else v
-        if given.dtype not in _KV8_TYPES:
+        kind = _KV8_TYPES.get(given.dtype)
+        if kind is None:
             raise TypeError("k and v must be float16 or bfloat16, got %s" % given.dtype)
         if k is not None and v is not None and k.shape != v.shape:
             raise ValueError("k and v must have the same shape")
         if n_rows is not None and n_rows != given.shape[0]:
             raise ValueError("n_rows is %d, the tensors have %d rows" % (n_rows, given.shape[0]))
-        kr, vr = (None if t is None else
-                  ctypes.byref(_kv8_rows(t, name, self.n_kv_heads, self.head_dim, given.dtype, self.device))
-                  for t, name in ((k, "k"), (v, "v")))
+        kr = None if k is None else _kv8_rows(k, "k", self.n_kv_heads, self.head_dim, given.dtype, self._index)
+        vr = None if v is None else _kv8_rows(v, "v", self.n_kv_heads, self.head_dim, given.dtype, self._index)
         batch = self._batch(block_table, kv_len, row_start, given.shape[0])
-        self._check(self.lib.h1b_kv8_read(self._pool_ref, ctypes.byref(batch), kr, vr, _KV8_TYPES[given.dtype],
-                                          stream.cuda_stream))
+        self._check(self.lib.h1b_kv8_read(self._pool_at, batch, kr, vr, kind, self._stream(stream)))
         return k, v
 
     def h1b_kv8_attention(self, q: torch.Tensor, block_table: torch.Tensor, kv_len: torch.Tensor, row_start: torch.Tensor,
@@ -570,29 +577,36 @@ class KV8Pages:
         """q: fp16 or bf16 CUDA [n_rows, Hq, d] -> out of q's dtype and shape; with return_lse (out, lse), lse fp32 [n_rows, Hq].
         window = 0: every token up to the row's own; else its last `window` and the sequence's first `sinks`. max_rows: the
         largest number of rows of one sequence, if the caller knows it (1 for a decode step); it only chooses kernels."""
-        dtype, device = q.dtype, self.device
-        if dtype not in _KV8_TYPES:
+        dtype, index = q.dtype, self._index
+        kind = _KV8_TYPES.get(dtype)
+        if kind is None:
             raise TypeError("q must be float16 or bfloat16, got %s" % dtype)
         if q.dim() != 3:
             raise ValueError("q must be [n_rows, Hq, d]")
-        n_rows, hq, _ = q.shape
-        qr = _kv8_rows(q, "q", hq, self.head_dim, dtype, device)
-        stream = self._stream(stream)
-        window, sinks, max_rows = _int32("window", window), _int32("sinks", sinks), _int32("max_rows", n_rows if max_rows is None else max_rows)
+        n_rows, hq, d = q.shape
+        qr = _kv8_rows(q, "q", hq, self.head_dim, dtype, index)
+        batch = self._batch(block_table, kv_len, row_start, n_rows)
+        sizes = (n_rows, hq, window, sinks, max_rows, block_table.shape)
+        need = self._workspaces.get(sizes)
+        if max_rows is None:
+            max_rows = n_rows
+        if need is None:
+            for what, x in (("window", window), ("sinks", sinks), ("max_rows", max_rows)):
+                _int32(what, x)
+            need = self.lib.h1b_kv8_attention_bytes(self._pool_at, batch, hq, window, sinks, max_rows)
+            if len(self._workspaces) >= 4096:
+                self._workspaces.clear()
+            self._workspaces[sizes] = need
         if out is None:
-            out = self._empty((n_rows, hq, self.head_dim), dtype, stream)
+            out = self._empty((n_rows, hq, d), dtype, stream)
         elif out.shape != q.shape:
             raise ValueError("out must have q's shape")
-        orow = _kv8_rows(out, "out", hq, self.head_dim, dtype, device)
-        batch = self._batch(block_table, kv_len, row_start, n_rows)
-        batch_ref = ctypes.byref(batch)
-        need = self.lib.h1b_kv8_attention_bytes(self._pool_ref, batch_ref, hq, window, sinks, max_rows)
+        orow = _kv8_rows(out, "out", hq, d, dtype, index)
         workspace = self._empty((need,), torch.uint8, stream) if need else None
         lse = self._empty((n_rows, hq), torch.float32, stream) if return_lse else None
         self._check(self.lib.h1b_kv8_attention(
-            self._pool_ref, batch_ref, ctypes.byref(qr), ctypes.byref(orow), None if lse is None else lse.data_ptr(), hq,
-            _KV8_TYPES[dtype], scale, window, sinks, max_rows, None if workspace is None else workspace.data_ptr(), need,
-            stream.cuda_stream))
+            self._pool_at, batch, qr, orow, None if lse is None else lse.data_ptr(), hq, kind, scale, window, sinks, max_rows,
+            None if workspace is None else workspace.data_ptr(), need, self._stream(stream)))
         return (out, lse) if return_lse else out
 
     def h1b_kv8_poll_status(self):

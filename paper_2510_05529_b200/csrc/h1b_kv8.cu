@@ -6,9 +6,10 @@ namespace h1b {
 namespace {
 
 // ------------------------------------------------------------------------------------------------------------------
-// Append and read. One row of d numbers is handled by d / 8 lanes (8 numbers, 16 bytes, each), keys and values side by
-// side in one warp; a warp takes `heads` KV heads of one row, so the walk over the batch and the page table is done once
-// for all of them.
+// Append and read. A row of d numbers is handled by d / 16 lanes (16 numbers, 32 bytes, each), the keys and values of two
+// (d = 128) or four heads side by side in one warp; a warp takes `heads` KV heads of one row, so the walk over the batch and
+// the page table is done once for all of them, and the next heads' loads are under way while it works on these. Both are
+// bound by memory: a token of a head is 2 * 2 d bytes on one side and 2 (d + 4) on the other.
 // ------------------------------------------------------------------------------------------------------------------
 struct Kv8Io {
     Kv8Params P;
@@ -27,111 +28,180 @@ __device__ __forceinline__ int64_t kv8_place(const Kv8Params &P, const Kv8Seq &s
     return (int64_t)page * P.hkv * P.page_tokens + (pos - col * P.page_tokens);
 }
 
-template <int D, int FMT>
-__global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Io io, const int bf16) {
-    constexpr int LANES = D / 8, VECS = 32 / LANES;              // lanes per vector, vectors (key or value rows) per warp
+// The codes of 16 numbers f and their row's amax. A code is the exact quotient TOP x / amax rounded once. TOP / amax is
+// rounded to fp32 (2^-24) and moved up and down by 2^-22, so the exact quotient lies between the two products: where both
+// round to the same code, that is the one. Elsewhere (one number in 10^4, and every tie) the lane divides: TOP x is exact in
+// fp32 (7 + 11 bits), the division is correctly rounded, and a quotient of such numbers that is not on a border between two
+// codes lies at least 2^-16 of itself away from it, so fp32 cannot put it there or across.
+template <int FMT>
+__device__ __forceinline__ uint4 kv8_quantise16(const float (&f)[16], float amax) {
     constexpr float TOP = FMT == H1B_KV8_INT8 ? 127.f : 448.f;
+    const float by = __fdiv_rn(TOP, amax), up = by * (1.f + 0x1p-22f), dn = by * (1.f - 0x1p-22f);
+    uint32_t c[4], differ = 0;
+    if (FMT == H1B_KV8_INT8) {
+        constexpr float MAGIC = 12582912.f;                      // 1.5 * 2^23: the integer nearest to x lands in the low byte of x + MAGIC
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t r[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                r[j] = __float_as_uint(fmaf(f[4 * i + j], up, MAGIC));
+                differ |= r[j] ^ __float_as_uint(fmaf(f[4 * i + j], dn, MAGIC));
+            }
+            c[i] = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint16_t h[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float x = f[4 * i + 2 * j], y = f[4 * i + 2 * j + 1];
+                uint16_t other;
+                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[j]) : "f"(y * up), "f"(x * up));
+                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(other) : "f"(y * dn), "f"(x * dn));
+                differ |= h[j] ^ other;
+            }
+            c[i] = h[0] | (uint32_t)h[1] << 16;
+        }
+    }
+    const bool near = differ != 0 || !(amax >= 0x1p-100f);       // (TOP / amax could overflow)
+    if (near) {
+        const float down = amax > 1e30f ? 0x1p-16f : 1.f, m = amax * down;   // TOP * x stays finite
+        uint32_t *w = c;
+#pragma unroll 1
+        for (int i = 0; i < 4; ++i) {
+            float q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float x = i == 0 ? f[j] : i == 1 ? f[4 + j] : i == 2 ? f[8 + j] : f[12 + j];
+                q[j] = __fdiv_rn(x * down * TOP, m);
+            }
+            uint32_t r;
+            if (FMT == H1B_KV8_INT8) {
+                r = ((uint32_t)__float2int_rn(q[0]) & 255u) | ((uint32_t)__float2int_rn(q[1]) & 255u) << 8 |
+                    ((uint32_t)__float2int_rn(q[2]) & 255u) << 16 | (uint32_t)__float2int_rn(q[3]) << 24;
+            } else {
+                uint16_t a, b;
+                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(a) : "f"(q[1]), "f"(q[0]));
+                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(q[3]), "f"(q[2]));
+                r = a | (uint32_t)b << 16;
+            }
+            if (i == 0) w[0] = r; else if (i == 1) w[1] = r; else if (i == 2) w[2] = r; else w[3] = r;
+        }
+    }
+    return make_uint4(c[0], c[1], c[2], c[3]);
+}
+
+template <int D, int FMT, bool BF16>
+__global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Io io) {
+    constexpr int LANES = D / 16, VECS = 32 / LANES;             // lanes per vector, vectors (key or value rows) per warp
+    constexpr float TOP = FMT == H1B_KV8_INT8 ? 127.f : 448.f;
+    constexpr uint32_t ODD = BF16 ? 0x7F80u : 0x7C00u;           // the bits of infinity: those of NaN are larger
     const Kv8Params &P = io.P;
-    const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    const int64_t r64 = unit / io.groups;
-    if (r64 >= P.n_rows) return;                                 // (whole warps)
-    const int r = (int)r64;
-    const int h0 = (int)(unit - r64 * io.groups) * io.heads, h1 = min(h0 + io.heads, P.hkv);
+    const int lane = threadIdx.x & 31, sub = lane % LANES;
+    const uint32_t unit = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    const int r = unit / io.groups;
+    if (r >= P.n_rows) return;                                   // (whole warps)
+    const int h0 = (int)(unit - (uint32_t)r * io.groups) * io.heads, h1 = min(h0 + io.heads, P.hkv);
+    // vector x of the row: head x / 2, its key (x even) or value
+    const uint16_t *src_k = static_cast<const uint16_t *>(io.k.data) + (int64_t)r * io.k.row_stride + sub * 16;
+    const uint16_t *src_v = static_cast<const uint16_t *>(io.v.data) + (int64_t)r * io.v.row_stride + sub * 16;
+    auto load = [&](int x, uint4 (&w)[2]) {
+        w[0] = w[1] = make_uint4(0, 0, 0, 0);
+        if ((x >> 1) >= h1) return;
+        const uint16_t *p = (x & 1) ? src_v + (int64_t)(x >> 1) * io.v.head_stride : src_k + (int64_t)(x >> 1) * io.k.head_stride;
+        w[0] = __ldcs(reinterpret_cast<const uint4 *>(p));
+        w[1] = __ldcs(reinterpret_cast<const uint4 *>(p) + 1);
+    };
+    uint4 next[2];
+    load(h0 * 2 + lane / LANES, next);                           // (nobody's rows lie in the tensors too)
     Kv8Seq s;
     if (!kv8_seq_of_row(P, r, lane, &s)) return;
     const int64_t at = kv8_place(P, s, r);
     if (at < 0) return;
-    const int sub = lane % LANES;
-    for (int x = h0 * 2 + lane / LANES; x < (h1 * 2 + VECS - 1) / VECS * VECS; x += VECS) {   // x = head * 2 + (0 key, 1 value)
-        const int h = x >> 1;
-        const bool live = h < h1;
-        const h1b_kv8_rows &src = (x & 1) ? io.v : io.k;
-        uint4 raw = make_uint4(0, 0, 0, 0);
-        if (live)
-            raw = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(src.data) + (int64_t)r * src.row_stride +
-                                                   (int64_t)h * src.head_stride + sub * 8);
-        float f[8];
-        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-        float amax = 0.f;
-        bool odd = false;                                        // an infinity or a NaN
+#pragma unroll 1
+    for (int x0 = h0 * 2; x0 < h1 * 2; x0 += VECS) {
+        const int x = x0 + lane / LANES, h = x >> 1;
+        const uint32_t w[8] = {next[0].x, next[0].y, next[0].z, next[0].w, next[1].x, next[1].y, next[1].z, next[1].w};
+        if (x0 + VECS < h1 * 2) load(x + VECS, next);
+        // magnitudes order as their bits do, infinities and NaN above all numbers
+        uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 p = pair_to_float2(w[i], bf16);
-            f[2 * i] = p.x; f[2 * i + 1] = p.y;
-            amax = fmaxf(amax, fmaxf(fabsf(p.x), fabsf(p.y)));
-            odd |= !(fabsf(p.x) <= 3.402823466e38f) || !(fabsf(p.y) <= 3.402823466e38f);
-        }
+        for (int i = 0; i < 8; ++i) top = __vmaxu2(top, w[i] & 0x7FFF7FFFu);
 #pragma unroll
-        for (int o = 1; o < LANES; o <<= 1) {
-            amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, o));
-            odd |= (bool)__shfl_xor_sync(~0u, (int)odd, o);
-        }
-        // TOP * x is exact in fp32 (7 + 11 bits) and the quotient correctly rounded; quotients of such numbers that are
-        // not ties lie at least 2^-16 of themselves away from one, so the codes are those of the exact quotient.
-        uint32_t lo = 0, hi = 0;
-        if (!odd && amax > 0.f) {
-            const float down = amax > 1e30f ? 0x1p-16f : 1.f, by = amax * down;   // TOP * x stays finite
-            float q[8];
+        for (int o = 1; o < LANES; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(~0u, top, o));
+        top = max(top >> 16, top & 0xFFFFu);
+        const bool odd = top >= ODD;                             // the row holds an infinity or a NaN
+        const float amax = pair_to_float2(top, BF16).x;
+        uint4 c = make_uint4(0, 0, 0, 0);
+        if (!odd && top) {
+            float f[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) q[i] = __fdiv_rn(f[i] * down * TOP, by);
-            if (FMT == H1B_KV8_INT8) {
-                uint32_t c[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) c[i] = (uint32_t)__float2int_rn(q[i]) & 255u;
-                lo = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
-                hi = c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24;
-            } else {
-                uint16_t c[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c[i]) : "f"(q[2 * i + 1]), "f"(q[2 * i]));
-                lo = c[0] | (uint32_t)c[1] << 16;
-                hi = c[2] | (uint32_t)c[3] << 16;
+            for (int i = 0; i < 8; ++i) {
+                const float2 p = pair_to_float2(w[i], BF16);
+                f[2 * i] = p.x; f[2 * i + 1] = p.y;
             }
+            c = kv8_quantise16<FMT>(f, amax);
         }
-        if (!live) continue;
-        const int64_t row = at + (int64_t)h * P.page_tokens;
-        *reinterpret_cast<uint2 *>(((x & 1) ? P.v : P.k) + row * D + sub * 8) = make_uint2(lo, hi);
-        if (sub == 0) ((x & 1) ? P.vs : P.ks)[row] = odd ? __int_as_float(0x7FC00000) : __fdiv_rn(amax, TOP);
+        if (h < h1) {
+            const int64_t row = at + (int64_t)h * P.page_tokens;
+            *reinterpret_cast<uint4 *>(((x & 1) ? P.v : P.k) + row * D + sub * 16) = c;
+            if (sub == 0) ((x & 1) ? P.vs : P.ks)[row] = odd ? __int_as_float(0x7FC00000) : __fdiv_rn(amax, TOP);
+        }
+        __syncwarp();
     }
 }
 
-template <int D, int FMT>
-__global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Io io, const int bf16) {
-    constexpr int LANES = D / 8, VECS = 32 / LANES;
+template <int D, int FMT, bool BF16>
+__global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Io io) {
+    constexpr int LANES = D / 16, VECS = 32 / LANES;
     const Kv8Params &P = io.P;
-    const int lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    const int64_t r64 = unit / io.groups;
-    if (r64 >= P.n_rows) return;
-    const int r = (int)r64;
-    const int h0 = (int)(unit - r64 * io.groups) * io.heads, h1 = min(h0 + io.heads, P.hkv);
+    const int lane = threadIdx.x & 31, sub = lane % LANES;
+    const uint32_t unit = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    const int r = unit / io.groups;
+    if (r >= P.n_rows) return;
+    const int h0 = (int)(unit - (uint32_t)r * io.groups) * io.heads, h1 = min(h0 + io.heads, P.hkv);
     Kv8Seq s;
     if (!kv8_seq_of_row(P, r, lane, &s)) return;
     const int64_t at = kv8_place(P, s, r);
-    const int sub = lane % LANES;
-    for (int x = h0 * 2 + lane / LANES; x < h1 * 2; x += VECS) {
-        const int h = x >> 1;
-        const h1b_kv8_rows &dst = (x & 1) ? io.v : io.k;
-        if (!dst.data) continue;
-        uint32_t w[4] = {0, 0, 0, 0};
-        if (at >= 0) {
-            const int64_t row = at + (int64_t)h * P.page_tokens;
-            const uint2 c = *reinterpret_cast<const uint2 *>(((x & 1) ? P.v : P.k) + row * D + sub * 8);
-            const float sc = ((x & 1) ? P.vs : P.ks)[row];
-            uint32_t hh[4];
-            kv8_codes4<FMT>(c.x, hh[0], hh[1]);
-            kv8_codes4<FMT>(c.y, hh[2], hh[3]);
+    auto load = [&](int x, uint4 &c, float &sc) {
+        c = make_uint4(0, 0, 0, 0);
+        sc = 0.f;                                                // (a token that is nowhere reads as zeros)
+        if (at < 0 || (x >> 1) >= h1) return;
+        const int64_t row = at + (int64_t)(x >> 1) * P.page_tokens;
+        c = __ldcs(reinterpret_cast<const uint4 *>(((x & 1) ? P.v : P.k) + row * D + sub * 16));
+        sc = ((x & 1) ? P.vs : P.ks)[row];
+    };
+    constexpr int AHEAD = 2;                                     // loads under way
+    uint4 c[AHEAD];
+    float sc[AHEAD];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 p = half2_bits_to_float2(hh[i]);
-                w[i] = float2_to_pair(p.x * sc, p.y * sc, bf16);
+    for (int i = 0; i < AHEAD; ++i) load(h0 * 2 + i * VECS + lane / LANES, c[i], sc[i]);
+#pragma unroll 1
+    for (int x0 = h0 * 2; x0 < h1 * 2; x0 += AHEAD * VECS)
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int x = x0 + i * VECS + lane / LANES, h = x >> 1;
+            const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+            const float by = sc[i];
+            load(x + AHEAD * VECS, c[i], sc[i]);
+            const h1b_kv8_rows &dst = (x & 1) ? io.v : io.k;
+            if (h >= h1 || !dst.data) continue;
+            uint32_t out[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t a, b;
+                kv8_codes4<FMT>(w[j], a, b);
+                const float2 p = half2_bits_to_float2(a), q = half2_bits_to_float2(b);
+                out[2 * j] = float2_to_pair(p.x * by, p.y * by, BF16);
+                out[2 * j + 1] = float2_to_pair(q.x * by, q.y * by, BF16);
             }
+            uint4 *to = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(dst.data) + (int64_t)r * dst.row_stride +
+                                                  (int64_t)h * dst.head_stride + sub * 16);
+            to[0] = make_uint4(out[0], out[1], out[2], out[3]);
+            to[1] = make_uint4(out[4], out[5], out[6], out[7]);
         }
-        *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(dst.data) + (int64_t)r * dst.row_stride +
-                                   (int64_t)h * dst.head_stride + sub * 8) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
 }
 
 template <bool APPEND>
@@ -139,20 +209,22 @@ cudaError_t launch_io(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_r
                       cudaStream_t st) {
     Kv8Io io;
     io.P = P; io.k = k; io.v = v;
-    // few rows: a warp per two vectors (latency); many: a warp takes up to eight heads
-    io.heads = 256 / d / 2;
-    while (io.heads < 8 && (int64_t)P.n_rows * ((P.hkv + io.heads - 1) / io.heads) > 148 * 64) io.heads *= 2;
+    // few rows: as few heads a warp as it has lanes for (latency); many: up to eight
+    io.heads = 32 / (d / 16) / 2;
+    while (io.heads < 8 && (int64_t)P.n_rows * ((P.hkv + io.heads - 1) / io.heads) > 148 * 128) io.heads *= 2;
     io.groups = (P.hkv + io.heads - 1) / io.heads;
     const int64_t warps = (int64_t)P.n_rows * io.groups;
     const int warps_per_block = warps < 148 * 8 ? 1 : 8;
     const unsigned grid = (unsigned)((warps + warps_per_block - 1) / warps_per_block);
-#define H1B_KV8_IO(D, F)                                                                          \
-    if (APPEND) kv8_append_kernel<D, F><<<grid, warps_per_block * 32, 0, st>>>(io, bf16);         \
-    else kv8_read_kernel<D, F><<<grid, warps_per_block * 32, 0, st>>>(io, bf16)
-    if (d == 128 && fmt == H1B_KV8_INT8) { H1B_KV8_IO(128, H1B_KV8_INT8); }
-    else if (d == 128) { H1B_KV8_IO(128, H1B_KV8_E4M3); }
-    else if (fmt == H1B_KV8_INT8) { H1B_KV8_IO(64, H1B_KV8_INT8); }
-    else { H1B_KV8_IO(64, H1B_KV8_E4M3); }
+#define H1B_KV8_IO(D, F, B)                                                                       \
+    if (APPEND) kv8_append_kernel<D, F, B><<<grid, warps_per_block * 32, 0, st>>>(io);            \
+    else kv8_read_kernel<D, F, B><<<grid, warps_per_block * 32, 0, st>>>(io)
+#define H1B_KV8_IO2(D, F) if (bf16) { H1B_KV8_IO(D, F, true); } else { H1B_KV8_IO(D, F, false); }
+    if (d == 128 && fmt == H1B_KV8_INT8) { H1B_KV8_IO2(128, H1B_KV8_INT8) }
+    else if (d == 128) { H1B_KV8_IO2(128, H1B_KV8_E4M3) }
+    else if (fmt == H1B_KV8_INT8) { H1B_KV8_IO2(64, H1B_KV8_INT8) }
+    else { H1B_KV8_IO2(64, H1B_KV8_E4M3) }
+#undef H1B_KV8_IO2
 #undef H1B_KV8_IO
     return cudaGetLastError();
 }
@@ -182,11 +254,31 @@ __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
     return r;
 }
 
+// Block p of this block's cluster: the number at the place where this block has `addr`.
+__device__ __forceinline__ uint32_t cluster_at(uint32_t addr, int p) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(p));
+    return r;
+}
+__device__ __forceinline__ float cluster_load(uint32_t addr, int p) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_at(addr, p)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float2 cluster_load2(uint32_t addr, int p) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(cluster_at(addr, p)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 template <int D>
 __host__ __device__ constexpr int rows_stage_bytes() { return 32 * D + 128; }
 template <int D, int NB>
 __host__ __device__ constexpr int rows_smem_bytes() {
-    const int ring = kRowsWarps * kRowsStages * rows_stage_bytes<D>(), merge = kRowsWarps * 8 * NB * (D + 2) * 4;
+    const int ring = kRowsWarps * kRowsStages * rows_stage_bytes<D>(), merge = kRowsWarps * 8 * NB * (D + 2) * 4 + 8 * NB * (D + 1) * 4;
     return ring > merge ? ring : merge;
 }
 
@@ -211,8 +303,8 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_ker
         // the tile's blocks in parts of `per`, a multiple of four (one per warp) and at least two per warp
         const int per = max((((span.count + A.splits - 1) / A.splits) + 3) & ~3, 2 * kRowsWarps);
         const int parts = max(1, (span.count + per - 1) / per);
-        if (split >= parts) continue;
-        const int j0 = split * per, j1 = min(j0 + per, span.count);
+        if (split >= parts && (parts == 1 || !A.cluster)) continue;
+        const int j0 = min(split * per, span.count), j1 = min(j0 + per, span.count);
         const int n_mine = j1 - j0 > warp ? (j1 - j0 - warp + kRowsWarps - 1) / kRowsWarps : 0;
 
         // ---- the copies: block i of this warp into stage i % 3; where the blocks lie is looked up 32 blocks at a time ----
@@ -472,10 +564,12 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_ker
             }
         }
         cp_async_wait_group<0>();
+        launch_dependents();
 
         // ---- the four warps' results meet in shared memory: [warp][row][d], then m and l [warp][row] ----
         __syncthreads();
         float *acc = reinterpret_cast<float *>(smem), *ml = acc + kRowsWarps * R * D;
+        float *res = ml + kRowsWarps * R * 2, *res_lse = res + R * D;   // this part's result, for the cluster
         const float unit = sigma * (1.f / kWeightUnit);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
@@ -516,16 +610,49 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_ker
             const bool empty = top == -INFINITY;
             if (empty) { a0 = a1 = 0.f; } else { a0 /= sum; a1 /= sum; }
             const int tok = (pair0 + row) / A.group, head = kvh * A.group + (pair0 + row) % A.group;
-            const int64_t part = (((int64_t)idx * P.hkv + kvh) * R + row) * A.splits + split;
             const float lse2 = empty ? -INFINITY : top + log2f(sum);
             if (parts == 1) {
                 *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(A.out) + (int64_t)(s.start + tok) * A.o_rs +
                                               (int64_t)head * A.o_hs + ch) = float2_to_pair(a0, a1, A.bf16);
                 if (A.lse && ch == 0) A.lse[(int64_t)(s.start + tok) * A.hq + head] = lse2 * kLn2;
+            } else if (A.cluster) {
+                *reinterpret_cast<float2 *>(res + row * D + ch) = make_float2(a0, a1);
+                if (ch == 0) res_lse[row] = lse2;
             } else {
+                const int64_t part = (((int64_t)idx * P.hkv + kvh) * R + row) * A.splits + split;
                 *reinterpret_cast<float2 *>(A.part_acc + part * D + ch) = make_float2(a0, a1);
                 if (ch == 0) A.part_lse[part] = lse2;
             }
+        }
+        if (A.cluster && parts > 1) {
+            // The parts of a tile are a cluster: they join in each other's shared memory, every block a share of the numbers.
+            // (All blocks of a cluster come through here for the same tiles.)
+            cluster_sync();
+            const uint32_t at = smem_addr(res), at_lse = smem_addr(res_lse);
+            for (int x = split * kRowsWarps * 32 + threadIdx.x; x < pairs * PER; x += A.splits * kRowsWarps * 32) {
+                const int row = x / PER, ch = (x % PER) * 2;
+                float top = -INFINITY, sum = 0.f, a0 = 0.f, a1 = 0.f;
+                bool nan = false;
+                for (int p = 0; p < parts; ++p) {
+                    const float y = cluster_load(at_lse + row * 4, p);
+                    top = fmaxf(top, y);
+                    nan |= y != y;
+                }
+                for (int p = 0; p < parts; ++p) {
+                    const float y = cluster_load(at_lse + row * 4, p), f = y == -INFINITY ? 0.f : ex2_approx(y - top);
+                    const float2 v = cluster_load2(at + (row * D + ch) * 4, p);
+                    sum += f;
+                    a0 += f * v.x;
+                    a1 += f * v.y;
+                }
+                const bool empty = top == -INFINITY && !nan;
+                const int tok = (pair0 + row) / A.group, head = kvh * A.group + (pair0 + row) % A.group;
+                *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(A.out) + (int64_t)(s.start + tok) * A.o_rs +
+                                              (int64_t)head * A.o_hs + ch) = empty ? 0u : float2_to_pair(a0 / sum, a1 / sum, A.bf16);
+                if (A.lse && ch == 0)
+                    A.lse[(int64_t)(s.start + tok) * A.hq + head] = empty ? -INFINITY : (top + log2f(sum)) * kLn2;
+            }
+            cluster_sync();                                      // nobody's results are overwritten or gone while another reads them
         }
         __syncthreads();                                         // the ring is free for the next tile's copies
     }
@@ -538,6 +665,7 @@ __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Params P, const 
                                                        const int min_blocks) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int idx = blockIdx.x / P.hkv, kvh = blockIdx.x % P.hkv;
+    grid_dependency_wait();                                      // launched while the attention kernel's last blocks run
     Kv8Seq s;
     int tile;
     if (!kv8_find_tile(P, A, idx, R, lane, &s, &tile)) return;
@@ -585,11 +713,22 @@ __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Params P, const 
 template <int D, int FMT, int NB, bool SPLIT>
 cudaError_t launch_rows_of(const Kv8Params &P, const Kv8Attn &A, int grid_tiles, cudaStream_t st) {
     constexpr int bytes = rows_smem_bytes<D, NB>();
-    const cudaError_t e = cudaFuncSetAttribute(kv8_rows_kernel<D, FMT, NB, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    static Kv8Once once;
+    const cudaError_t e = once.shared_memory(reinterpret_cast<const void *>(kv8_rows_kernel<D, FMT, NB, SPLIT>), bytes);
     if (e != cudaSuccess) return e;
-    const dim3 grid((unsigned)grid_tiles, (unsigned)P.hkv, (unsigned)A.splits);
-    kv8_rows_kernel<D, FMT, NB, SPLIT><<<grid, kRowsWarps * 32, bytes, st>>>(P, A);
-    return cudaGetLastError();
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 1;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = (unsigned)A.splits;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid_tiles, (unsigned)P.hkv, (unsigned)A.splits);
+    cfg.blockDim = dim3(kRowsWarps * 32);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = A.cluster ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kv8_rows_kernel<D, FMT, NB, SPLIT>, P, A);
 }
 
 }  // namespace
@@ -614,16 +753,23 @@ cudaError_t launch_kv8_rows(const Kv8Params &P, const Kv8Attn &A, int d, int fmt
     else if (fmt == H1B_KV8_INT8) { H1B_KV8_ROWS(64, H1B_KV8_INT8); }
     else { H1B_KV8_ROWS(64, H1B_KV8_E4M3); }
 #undef H1B_KV8_ROWS
-    if (e != cudaSuccess || A.splits == 1) return e;
+    if (e != cudaSuccess || A.splits == 1 || A.cluster) return e;
     return launch_kv8_join(P, A, d, rows_per_tile, kRowsWarps, 2 * kRowsWarps, st);
 }
 
 cudaError_t launch_kv8_join(const Kv8Params &P, const Kv8Attn &A, int d, int rows_per_tile, int unit_blocks, int min_blocks,
                             cudaStream_t st) {
-    const dim3 grid((unsigned)A.tiles * (unsigned)P.hkv, (unsigned)(rows_per_tile / 8));
-    if (d == 128) kv8_join_kernel<128><<<grid, 128, 0, st>>>(P, A, rows_per_tile, unit_blocks, min_blocks);
-    else kv8_join_kernel<64><<<grid, 128, 0, st>>>(P, A, rows_per_tile, unit_blocks, min_blocks);
-    return cudaGetLastError();
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)A.tiles * (unsigned)P.hkv, (unsigned)(rows_per_tile / 8));
+    cfg.blockDim = dim3(128);
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return d == 128 ? cudaLaunchKernelEx(&cfg, kv8_join_kernel<128>, P, A, rows_per_tile, unit_blocks, min_blocks)
+                    : cudaLaunchKernelEx(&cfg, kv8_join_kernel<64>, P, A, rows_per_tile, unit_blocks, min_blocks);
 }
 
 }  // namespace h1b

@@ -1,6 +1,7 @@
 // 8-bit pages (h1b_kv8_*): what the append / read / attention kernels share. Parameter blocks, the walk over a ragged
 // batch, and the conversion of 8-bit codes to fp16 operands.
 #pragma once
+#include <atomic>
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -38,6 +39,7 @@ struct Kv8Attn {
     int tiles;                             // no batch of n_rows rows has more tiles than this
     int min_pairs;                         // sequences with fewer (row, head of the group) pairs are another kernel's ...
     int max_pairs;                         // ... and those with more
+    int cluster;                           // few rows: the parts of a tile are a cluster and join by themselves
     float *part_acc, *part_lse;            // [tiles][hkv][pairs of a tile][splits] times [d], and alone (log2)
 };
 
@@ -189,6 +191,21 @@ __device__ __forceinline__ int kv8_row_exponent(float amax) {
     const int e = (int)(__float_as_uint(amax) >> 23) - 127 - 14;   // (a subnormal amax: -141, clamped)
     return clampi(e, -100, 113);
 }
+
+// A kernel's launch attribute, set once on each device (again if two threads meet: it is the same value).
+struct Kv8Once {
+    std::atomic<uint64_t> done{0};
+    cudaError_t shared_memory(const void *kernel, int bytes) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+        if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+        return e;
+    }
+};
 
 cudaError_t launch_kv8_append(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_rows &v, int d, int fmt, int bf16,
                               cudaStream_t st);

@@ -112,6 +112,8 @@ int check_io(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8
     if (rc == H1B_OK) rc = check_rows("k", k, batch->n_rows, pool->n_kv_heads, pool->head_dim, output, output);
     if (rc == H1B_OK) rc = check_rows("v", v, batch->n_rows, pool->n_kv_heads, pool->head_dim, output, output);
     if (rc == H1B_OK) rc = check_type(dtype);
+    if (rc == H1B_OK && (int64_t)batch->n_rows * pool->n_kv_heads >= (int64_t)1 << 31)
+        return report_error(H1B_ERR_INVALID_ARG, "n_rows * n_kv_heads reaches 2^31");
     return rc;
 }
 
@@ -121,7 +123,7 @@ int check_io(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8
 constexpr int kFewPairs = 32;
 
 struct AttnPart {
-    bool used = false;
+    bool used = false, cluster = false;
     int rows_per_tile = 0, tiles = 0, grid_tiles = 0, splits = 1, min_pairs = 1, max_pairs = 1 << 30;
     size_t lines = 0;                                            // partial results
 };
@@ -148,24 +150,33 @@ AttnPlan plan_of(const h1b_kv8_pool *p, const h1b_kv8_batch *b, int hq, int wind
         f.tiles = (int)(pairs / f.rows_per_tile + seqs);
         if (a.many.used) f.tiles = (int)std::min<int64_t>(f.tiles, hinted);    // (no sequence has more)
         f.grid_tiles = (int)std::min<int64_t>(f.tiles, hinted);
-        // Parts: enough blocks for four waves of the GPU's 148 SMs at three blocks an SM, so that ragged lengths even out;
-        // no more than the tokens that a row can see give work to (two blocks of 16 tokens a warp, four warps).
-        const int64_t blocks = (int64_t)f.grid_tiles * p->n_kv_heads;
-        // (The last limit bounds the workspace when max_rows says far less than the batch holds.)
-        f.splits = (int)std::max<int64_t>(1, std::min<int64_t>({(148 * 12 + blocks - 1) / blocks, (seen + 127) / 128, 256,
-                                                                148 * 48 / ((int64_t)f.tiles * p->n_kv_heads)}));
+        // Parts. The GPU holds 148 * 4 blocks of 8-row tiles at once (half as many of 16 rows). Fill it once, as far as there
+        // are 128 tokens for each block (two blocks of 16 a warp); go to four times as many blocks, so that ragged lengths
+        // even out, where each still has 1024 tokens (more and shorter ones cost: 32 sequences with a window of 1024 tokens
+        // took 24 us in seven parts and 16 in two). The last limit bounds the workspace when max_rows says far less than the
+        // batch holds.
+        const int64_t blocks = (int64_t)f.grid_tiles * p->n_kv_heads, slots = f.rows_per_tile == 8 ? 148 * 4 : 148 * 2;
+        const int64_t fill = std::min<int64_t>(slots / blocks, (seen + 127) / 128), even = std::min<int64_t>(4 * slots / blocks, seen / 1024);
+        f.splits = (int)std::max<int64_t>(1, std::min<int64_t>({std::max(fill, even), 256, 148 * 48 / ((int64_t)f.tiles * p->n_kv_heads)}));
+        // Up to eight parts (the largest cluster that every GPU takes) join through each other's shared memory, others through
+        // the workspace and a kernel of its own, some 2 us more (one sequence of 777 tokens: 6.7 and 8.6 us). Blocks that come
+        // in several waves do better without clusters, whose parts start and end together (16 sequences of 4-8k tokens, 32
+        // heads: 155 us with, 150 without).
+        f.cluster = f.splits > 1 && f.splits <= 8 && blocks * f.splits <= slots;
     }
     if (a.many.used) {
         AttnPart &m = a.many;
         if (a.few.used) m.min_pairs = kFewPairs + 1;
         m.rows_per_tile = 256;
         m.tiles = m.grid_tiles = (int)(pairs / 256 + seqs);
-        // Parts only where there are too few tiles for the SMs, and of at least 512 tokens
+        // Parts only where there are too few tiles for the SMs (one block an SM): up to three times as many blocks as SMs, so
+        // that ragged lengths even out, each of at least 512 tokens (six sequences with 5 to 131 rows over 1-9k tokens: 206 us
+        // at one block an SM, 172, 163 and 163 at two, three and four, 180 at six).
         const int64_t blocks = (int64_t)m.tiles * p->n_kv_heads;
-        m.splits = blocks >= 148 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(296 / blocks, seen / 512));
+        m.splits = blocks >= 148 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(3 * 148 / blocks, seen / 512));
     }
     for (AttnPart *part : {&a.few, &a.many})
-        if (part->used && part->splits > 1) {
+        if (part->used && part->splits > 1 && !part->cluster) {
             part->lines = (size_t)part->tiles * p->n_kv_heads * part->rows_per_tile * part->splits;
             a.bytes += part->lines * (p->head_dim + 1) * sizeof(float);
         }
@@ -249,6 +260,7 @@ int h1b_kv8_attention(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, cons
     float *at = static_cast<float *>(workspace);
     auto take = [&](const AttnPart &part) {                      // this part's share of the workspace
         A.splits = part.splits; A.tiles = part.tiles; A.min_pairs = part.min_pairs; A.max_pairs = part.max_pairs;
+        A.cluster = part.cluster;
         A.part_acc = part.lines ? at : nullptr;
         A.part_lse = part.lines ? at + part.lines * pool->head_dim : nullptr;
         if (part.lines) at += part.lines * (pool->head_dim + 1);

@@ -725,7 +725,8 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
 template <int D, int FMT, bool SPLIT>
 cudaError_t launch_of(const Kv8Params &P, const Kv8Attn &A, cudaStream_t st) {
     constexpr int bytes = TlSmem<D>::kTotal;
-    const cudaError_t e = cudaFuncSetAttribute(kv8_tiles_kernel<D, FMT, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    static Kv8Once once;
+    const cudaError_t e = once.shared_memory(reinterpret_cast<const void *>(kv8_tiles_kernel<D, FMT, SPLIT>), bytes);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)A.tiles * (unsigned)P.hkv, 1, (unsigned)A.splits);
     kv8_tiles_kernel<D, FMT, SPLIT><<<grid, kTlThreads, bytes, st>>>(P, A);

@@ -105,6 +105,8 @@ def test_bad_numbers(so):
     assert so.h1b_kv8_attention(r(pool()), r(batch()), None, r(rows()), None, 4, 0, 0.1, 0, 0, 1, P, 1 << 40, None) == -2
     big = batch(n_rows=2 ** 29)
     assert attention(so, b=big) == -1
+    assert so.h1b_kv8_append(r(pool()), r(batch(n_rows=2 ** 30)), r(rows(row_stride=0)), r(rows(row_stride=0)), 0, None) == -1
+    assert so.h1b_kv8_append(r(pool(n_pages=2 ** 31 - 1)), r(batch()), r(rows()), r(rows()), 0, None) == -3
 
 
 def test_workspace_is_checked(so):
@@ -135,12 +137,24 @@ def test_the_python_binding_refuses():
         binding.KV8Pages(cpu, cpu, s, s)
     with pytest.raises(ValueError):
         binding._int32("window", 2 ** 31)
+    rows3 = torch.zeros(3, 2, 64)
     with pytest.raises(TypeError):
-        binding._kv8_rows(torch.zeros(3, 2, 64), "q", 2, 64, torch.float16, torch.device("cpu"))
+        binding._kv8_rows(rows3, "q", 2, 64, torch.float16, -1)
+    with pytest.raises(TypeError):
+        binding._kv8_rows(rows3, "q", 2, 64, torch.float32, 0)
     with pytest.raises(ValueError):
-        binding._kv8_rows(torch.zeros(3, 2, 64).transpose(1, 2), "q", 64, 2, torch.float32, torch.device("cpu"))
+        binding._kv8_rows(rows3.transpose(1, 2), "q", 64, 2, torch.float32, -1)
     with pytest.raises(ValueError):
-        binding._kv8_rows(torch.zeros(3, 2, 64), "q", 4, 64, torch.float32, torch.device("cpu"))
+        binding._kv8_rows(rows3, "q", 4, 64, torch.float32, -1)
+
+
+def test_the_structures_packed_by_hand_are_the_header_s():
+    """The binding packs h1b_kv8_rows and h1b_kv8_batch itself (it is faster): the same bytes as ctypes would lay out."""
+    t = torch.zeros(5, 4, 64)[:, ::2]
+    assert binding._kv8_rows(t, "q", 2, 64, torch.float32, -1) == bytes(binding.h1b_kv8_rows(t.data_ptr(), 256, 128))
+    packed = binding._BATCH(1, 2, 3, 4, 5, 6, 7)
+    assert packed == bytes(binding.h1b_kv8_batch(1, 2, 3, 4, 5, 6, 7)) and len(packed) == ctypes.sizeof(binding.h1b_kv8_batch)
+    assert binding._ROWS(1, -2, 3) == bytes(binding.h1b_kv8_rows(1, -2, 3))
 
 
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
