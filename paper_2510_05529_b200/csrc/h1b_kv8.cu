@@ -6,7 +6,8 @@ namespace h1b {
 namespace {
 
 // ------------------------------------------------------------------------------------------------------------------
-// Append and read. A row of d numbers is handled by d / 16 lanes (16 numbers, 32 bytes, each), the keys and values of two
+// Append and read. A row of d numbers is handled by d / 16 lanes (8 numbers of each half of the row, so that neighbouring
+// lanes read and write neighbouring bytes), the keys and values of two
 // (d = 128) or four heads side by side in one warp; a warp takes `heads` KV heads of one row, so the walk over the batch and
 // the page table is done once for all of them, and the next heads' loads are under way while it works on these. Both are
 // bound by memory: a token of a head is 2 * 2 d bytes on one side and 2 (d + 4) on the other.
@@ -28,56 +29,55 @@ __device__ __forceinline__ int64_t kv8_place(const Kv8Params &P, const Kv8Seq &s
     return (int64_t)page * P.hkv * P.page_tokens + (pos - col * P.page_tokens);
 }
 
-// The codes of 16 numbers f and their row's amax. A code is the exact quotient TOP x / amax rounded once. TOP / amax is
-// rounded to fp32 (2^-24) and moved up and down by 2^-22, so the exact quotient lies between the two products: where both
-// round to the same code, that is the one. Elsewhere (one number in 10^4, and every tie) the lane divides: TOP x is exact in
-// fp32 (7 + 11 bits), the division is correctly rounded, and a quotient of such numbers that is not on a border between two
-// codes lies at least 2^-16 of itself away from it, so fp32 cannot put it there or across.
+// The codes of 16 numbers f and their row's amax. A code is the exact quotient TOP x / amax rounded once. TOP / amax,
+// off by 2^-22 of itself at most, is moved up and down by 2^-21, so the exact quotient lies between the two products: where
+// both round to the same code, that is the one. Elsewhere (one number in 5000, most of them ties) the lane divides: TOP x is
+// exact in fp32 (7 + 11 bits), the division is correctly rounded, and a quotient of such numbers that is not on a border
+// between two codes lies at least 2^-16 of itself away from it, so fp32 cannot put it there or across.
+constexpr float kMagic = 12582912.f;                             // 1.5 * 2^23: the integer nearest to x lands in the low byte of x + kMagic
+template <int FMT>
+__device__ __forceinline__ uint32_t kv8_quantise4(float x, float y, float z, float w, float up, float dn, uint32_t &differ) {
+    if (FMT == H1B_KV8_INT8) {
+        const uint64_t f[2] = {pack2f(x, y), pack2f(z, w)}, magic = pack2f(kMagic, kMagic);
+        uint32_t r[4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float2 a = unpack2(fma2(f[j], pack2f(up, up), magic)), b = unpack2(fma2(f[j], pack2f(dn, dn), magic));
+            r[2 * j] = __float_as_uint(a.x);
+            r[2 * j + 1] = __float_as_uint(a.y);
+            differ |= (r[2 * j] ^ __float_as_uint(b.x)) | (r[2 * j + 1] ^ __float_as_uint(b.y));
+        }
+        return __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
+    }
+    uint16_t a, b, c, d;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(a) : "f"(y * up), "f"(x * up));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(y * dn), "f"(x * dn));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(w * up), "f"(z * up));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(d) : "f"(w * dn), "f"(z * dn));
+    differ |= (uint32_t)(a ^ b) | (uint32_t)(c ^ d);
+    return a | (uint32_t)c << 16;
+}
 template <int FMT>
 __device__ __forceinline__ uint4 kv8_quantise16(const float (&f)[16], float amax) {
     constexpr float TOP = FMT == H1B_KV8_INT8 ? 127.f : 448.f;
-    const float by = __fdiv_rn(TOP, amax), up = by * (1.f + 0x1p-22f), dn = by * (1.f - 0x1p-22f);
+    const float by = __fdividef(TOP, amax), up = by * (1.f + 0x1p-21f), dn = by * (1.f - 0x1p-21f);   // (off by 2 ulp at most)
     uint32_t c[4], differ = 0;
-    if (FMT == H1B_KV8_INT8) {
-        constexpr float MAGIC = 12582912.f;                      // 1.5 * 2^23: the integer nearest to x lands in the low byte of x + MAGIC
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t r[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                r[j] = __float_as_uint(fmaf(f[4 * i + j], up, MAGIC));
-                differ |= r[j] ^ __float_as_uint(fmaf(f[4 * i + j], dn, MAGIC));
-            }
-            c[i] = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint16_t h[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float x = f[4 * i + 2 * j], y = f[4 * i + 2 * j + 1];
-                uint16_t other;
-                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h[j]) : "f"(y * up), "f"(x * up));
-                asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(other) : "f"(y * dn), "f"(x * dn));
-                differ |= h[j] ^ other;
-            }
-            c[i] = h[0] | (uint32_t)h[1] << 16;
-        }
-    }
-    const bool near = differ != 0 || !(amax >= 0x1p-100f);       // (TOP / amax could overflow)
-    if (near) {
+    for (int i = 0; i < 4; ++i) c[i] = kv8_quantise4<FMT>(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3], up, dn, differ);
+    const bool wide = !(amax >= 0x1p-100f && amax <= 0x1p100f);  // where the quotient above is not that exact
+    if (differ || wide) {
         const float down = amax > 1e30f ? 0x1p-16f : 1.f, m = amax * down;   // TOP * x stays finite
-        uint32_t *w = c;
 #pragma unroll 1
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; ++i) {                            // a word at a time: the others are right
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = i == 0 ? f[j] : i == 1 ? f[4 + j] : i == 2 ? f[8 + j] : f[12 + j];
+            uint32_t again = 0, r;
+            (void)kv8_quantise4<FMT>(x[0], x[1], x[2], x[3], up, dn, again);
+            if (!again && !wide) continue;
             float q[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float x = i == 0 ? f[j] : i == 1 ? f[4 + j] : i == 2 ? f[8 + j] : f[12 + j];
-                q[j] = __fdiv_rn(x * down * TOP, m);
-            }
-            uint32_t r;
+            for (int j = 0; j < 4; ++j) q[j] = __fdiv_rn(x[j] * down * TOP, m);
             if (FMT == H1B_KV8_INT8) {
                 r = ((uint32_t)__float2int_rn(q[0]) & 255u) | ((uint32_t)__float2int_rn(q[1]) & 255u) << 8 |
                     ((uint32_t)__float2int_rn(q[2]) & 255u) << 16 | (uint32_t)__float2int_rn(q[3]) << 24;
@@ -87,17 +87,23 @@ __device__ __forceinline__ uint4 kv8_quantise16(const float (&f)[16], float amax
                 asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(q[3]), "f"(q[2]));
                 r = a | (uint32_t)b << 16;
             }
-            if (i == 0) w[0] = r; else if (i == 1) w[1] = r; else if (i == 2) w[2] = r; else w[3] = r;
+            if (i == 0) c[0] = r; else if (i == 1) c[1] = r; else if (i == 2) c[2] = r; else c[3] = r;
         }
     }
     return make_uint4(c[0], c[1], c[2], c[3]);
+}
+
+// The largest magnitude; NaN if there is one.
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+    float r;
+    asm("{\n\t.reg .f32 b, c;\n\tabs.f32 b, %2;\n\tabs.f32 c, %3;\n\tmax.NaN.f32 %0, %1, b, c;\n\t}" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 
 template <int D, int FMT, bool BF16>
 __global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Io io) {
     constexpr int LANES = D / 16, VECS = 32 / LANES;             // lanes per vector, vectors (key or value rows) per warp
     constexpr float TOP = FMT == H1B_KV8_INT8 ? 127.f : 448.f;
-    constexpr uint32_t ODD = BF16 ? 0x7F80u : 0x7C00u;           // the bits of infinity: those of NaN are larger
     const Kv8Params &P = io.P;
     const int lane = threadIdx.x & 31, sub = lane % LANES;
     const uint32_t unit = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
@@ -105,14 +111,14 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Io io) {
     if (r >= P.n_rows) return;                                   // (whole warps)
     const int h0 = (int)(unit - (uint32_t)r * io.groups) * io.heads, h1 = min(h0 + io.heads, P.hkv);
     // vector x of the row: head x / 2, its key (x even) or value
-    const uint16_t *src_k = static_cast<const uint16_t *>(io.k.data) + (int64_t)r * io.k.row_stride + sub * 16;
-    const uint16_t *src_v = static_cast<const uint16_t *>(io.v.data) + (int64_t)r * io.v.row_stride + sub * 16;
+    const uint16_t *src_k = static_cast<const uint16_t *>(io.k.data) + (int64_t)r * io.k.row_stride + sub * 8;
+    const uint16_t *src_v = static_cast<const uint16_t *>(io.v.data) + (int64_t)r * io.v.row_stride + sub * 8;
     auto load = [&](int x, uint4 (&w)[2]) {
         w[0] = w[1] = make_uint4(0, 0, 0, 0);
         if ((x >> 1) >= h1) return;
         const uint16_t *p = (x & 1) ? src_v + (int64_t)(x >> 1) * io.v.head_stride : src_k + (int64_t)(x >> 1) * io.k.head_stride;
         w[0] = __ldcs(reinterpret_cast<const uint4 *>(p));
-        w[1] = __ldcs(reinterpret_cast<const uint4 *>(p) + 1);
+        w[1] = __ldcs(reinterpret_cast<const uint4 *>(p + D / 2));
     };
     uint4 next[2];
     load(h0 * 2 + lane / LANES, next);                           // (nobody's rows lie in the tensors too)
@@ -125,28 +131,23 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Io io) {
         const int x = x0 + lane / LANES, h = x >> 1;
         const uint32_t w[8] = {next[0].x, next[0].y, next[0].z, next[0].w, next[1].x, next[1].y, next[1].z, next[1].w};
         if (x0 + VECS < h1 * 2) load(x + VECS, next);
-        // magnitudes order as their bits do, infinities and NaN above all numbers
-        uint32_t top = 0;
+        float f[16], amax = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = __vmaxu2(top, w[i] & 0x7FFF7FFFu);
-#pragma unroll
-        for (int o = 1; o < LANES; o <<= 1) top = __vmaxu2(top, __shfl_xor_sync(~0u, top, o));
-        top = max(top >> 16, top & 0xFFFFu);
-        const bool odd = top >= ODD;                             // the row holds an infinity or a NaN
-        const float amax = pair_to_float2(top, BF16).x;
-        uint4 c = make_uint4(0, 0, 0, 0);
-        if (!odd && top) {
-            float f[16];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float2 p = pair_to_float2(w[i], BF16);
-                f[2 * i] = p.x; f[2 * i + 1] = p.y;
-            }
-            c = kv8_quantise16<FMT>(f, amax);
+        for (int i = 0; i < 8; ++i) {
+            const float2 p = pair_to_float2(w[i], BF16);
+            f[2 * i] = p.x; f[2 * i + 1] = p.y;
+            amax = max_abs(amax, p.x, p.y);
         }
+#pragma unroll
+        for (int o = 1; o < LANES; o <<= 1) amax = max_abs(amax, amax, __shfl_xor_sync(~0u, amax, o));
+        const bool odd = !(amax <= 3.402823466e38f);             // the row holds an infinity or a NaN
+        uint4 c = make_uint4(0, 0, 0, 0);
+        if (!odd && amax > 0.f) c = kv8_quantise16<FMT>(f, amax);
         if (h < h1) {
             const int64_t row = at + (int64_t)h * P.page_tokens;
-            *reinterpret_cast<uint4 *>(((x & 1) ? P.v : P.k) + row * D + sub * 16) = c;
+            uint8_t *to = ((x & 1) ? P.v : P.k) + row * D + sub * 8;
+            *reinterpret_cast<uint2 *>(to) = make_uint2(c.x, c.y);
+            *reinterpret_cast<uint2 *>(to + D / 2) = make_uint2(c.z, c.w);
             if (sub == 0) ((x & 1) ? P.vs : P.ks)[row] = odd ? __int_as_float(0x7FC00000) : __fdiv_rn(amax, TOP);
         }
         __syncwarp();
@@ -170,10 +171,12 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Io io) {
         sc = 0.f;                                                // (a token that is nowhere reads as zeros)
         if (at < 0 || (x >> 1) >= h1) return;
         const int64_t row = at + (int64_t)(x >> 1) * P.page_tokens;
-        c = __ldcs(reinterpret_cast<const uint4 *>(((x & 1) ? P.v : P.k) + row * D + sub * 16));
+        const uint8_t *from = ((x & 1) ? P.v : P.k) + row * D + sub * 8;
+        const uint2 a = __ldcs(reinterpret_cast<const uint2 *>(from)), b = __ldcs(reinterpret_cast<const uint2 *>(from + D / 2));
+        c = make_uint4(a.x, a.y, b.x, b.y);
         sc = ((x & 1) ? P.vs : P.ks)[row];
     };
-    constexpr int AHEAD = 2;                                     // loads under way
+    constexpr int AHEAD = 4;                                     // loads under way
     uint4 c[AHEAD];
     float sc[AHEAD];
 #pragma unroll
@@ -198,9 +201,9 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Io io) {
                 out[2 * j + 1] = float2_to_pair(q.x * by, q.y * by, BF16);
             }
             uint4 *to = reinterpret_cast<uint4 *>(static_cast<uint16_t *>(dst.data) + (int64_t)r * dst.row_stride +
-                                                  (int64_t)h * dst.head_stride + sub * 16);
+                                                  (int64_t)h * dst.head_stride + sub * 8);
             to[0] = make_uint4(out[0], out[1], out[2], out[3]);
-            to[1] = make_uint4(out[4], out[5], out[6], out[7]);
+            to[D / 16] = make_uint4(out[4], out[5], out[6], out[7]);
         }
 }
 
