@@ -507,7 +507,7 @@ typedef struct {
     const int32_t *kv_len;      /* DEVICE [n_seqs]: cached tokens, new ones included */
     const int32_t *row_start;   /* DEVICE [n_seqs + 1]                               */
     int32_t *status;            /* DEVICE [1], nullable                              */
-    int32_t n_seqs;             /* >= 0                                              */
+    int32_t n_seqs;             /* 0 .. 2^20                                         */
     int32_t table_width;        /* >= 1; table_width * page_tokens <= 2^30           */
     int32_t n_rows;             /* rows in the call's tensors, >= 0                  */
 } h1b_kv8_batch;

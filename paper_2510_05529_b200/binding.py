@@ -500,6 +500,7 @@ class KV8Pages:
         self.device = k_pages.device
         n_pages, self.n_kv_heads, page_tokens, self.head_dim = (int(x) for x in k_pages.shape)
         self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        torch.cuda.current_stream(self.device).synchronize()   # (the first call may be on another stream)
         self._status = self.status.data_ptr()
         self._pool = h1b_kv8_pool(k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), n_pages,
                                   self.n_kv_heads, page_tokens, self.head_dim, _KV8_FORMATS[k_pages.dtype],
@@ -610,10 +611,13 @@ class KV8Pages:
         return (out, lse) if return_lse else out
 
     def h1b_kv8_poll_status(self):
-        """Synchronises; raises H1BError if a kernel met something in a batch that does not fit (see h1b_kv8_batch), and clears it."""
+        """Waits for the device; raises H1BError if a kernel met something in a batch that does not fit (see h1b_kv8_batch in
+        include/h1b.h), and clears it."""
+        torch.cuda.synchronize(self.device)
         code = int(self.status.item())
         if code != H1B_OK:
             self.status.zero_()
+            torch.cuda.synchronize(self.device)
             raise H1BError(code, "reported by a kernel of an h1b_kv8_ call")
 
 

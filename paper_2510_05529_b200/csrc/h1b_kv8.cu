@@ -1,4 +1,6 @@
 // 8-bit pages: quantise-and-append, read-back, and attention for few rows per sequence (decode steps, short chunks).
+#include <type_traits>
+
 #include "h1b_kv8.cuh"
 
 namespace h1b {
@@ -214,22 +216,18 @@ cudaError_t launch_io(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_r
     io.P = P; io.k = k; io.v = v;
     // few rows: as few heads a warp as it has lanes for (latency); many: up to eight
     io.heads = 32 / (d / 16) / 2;
-    while (io.heads < 8 && (int64_t)P.n_rows * ((P.hkv + io.heads - 1) / io.heads) > 148 * 128) io.heads *= 2;
+    while (io.heads < 8 && (int64_t)P.n_rows * ((P.hkv + io.heads - 1) / io.heads) > 148 * 64) io.heads *= 2;
     io.groups = (P.hkv + io.heads - 1) / io.heads;
     const int64_t warps = (int64_t)P.n_rows * io.groups;
     const int warps_per_block = warps < 148 * 8 ? 1 : 8;
     const unsigned grid = (unsigned)((warps + warps_per_block - 1) / warps_per_block);
-#define H1B_KV8_IO(D, F, B)                                                                       \
-    if (APPEND) kv8_append_kernel<D, F, B><<<grid, warps_per_block * 32, 0, st>>>(io);            \
-    else kv8_read_kernel<D, F, B><<<grid, warps_per_block * 32, 0, st>>>(io)
-#define H1B_KV8_IO2(D, F) if (bf16) { H1B_KV8_IO(D, F, true); } else { H1B_KV8_IO(D, F, false); }
-    if (d == 128 && fmt == H1B_KV8_INT8) { H1B_KV8_IO2(128, H1B_KV8_INT8) }
-    else if (d == 128) { H1B_KV8_IO2(128, H1B_KV8_E4M3) }
-    else if (fmt == H1B_KV8_INT8) { H1B_KV8_IO2(64, H1B_KV8_INT8) }
-    else { H1B_KV8_IO2(64, H1B_KV8_E4M3) }
+#define H1B_KV8_IO(D, F, B)                                                                                            \
+    kv8_launch(APPEND ? kv8_append_kernel<D, F, B> : kv8_read_kernel<D, F, B>, dim3(grid), warps_per_block * 32, 0, st, io)
+#define H1B_KV8_IO2(D, F) (bf16 ? H1B_KV8_IO(D, F, true) : H1B_KV8_IO(D, F, false))
+    if (d == 128) return fmt == H1B_KV8_INT8 ? H1B_KV8_IO2(128, H1B_KV8_INT8) : H1B_KV8_IO2(128, H1B_KV8_E4M3);
+    return fmt == H1B_KV8_INT8 ? H1B_KV8_IO2(64, H1B_KV8_INT8) : H1B_KV8_IO2(64, H1B_KV8_E4M3);
 #undef H1B_KV8_IO2
 #undef H1B_KV8_IO
-    return cudaGetLastError();
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -294,17 +292,21 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_ker
     const int kvh = blockIdx.y, split = blockIdx.z;
     const uint32_t ring = smem_addr(smem) + warp * kRowsStages * STAGE;
 
-    for (int idx = blockIdx.x; idx < A.tiles; idx += gridDim.x) {
-        Kv8Seq s;
-        int tile;
-        if (!kv8_find_tile(P, A, idx, R, lane, &s, &tile)) break;
+    // Blocks x * tiles .. + tiles - 1 belong to sequence x, one for each of its tiles; if it has more than the host said, they
+    // take those too, undivided.
+    const Kv8Seq s = kv8_seq(P, blockIdx.x / A.tiles);
+    if (s.n * A.group < A.min_pairs || s.n * A.group > A.max_pairs) return;
+    const int first_tile = blockIdx.x % A.tiles;
+    for (int tile = first_tile; tile * R < s.n * A.group; tile += A.tiles) {
+        const bool extra = tile != first_tile;
+        const int splits = extra ? 1 : A.splits;
         const int pair0 = tile * R, pairs = min(R, s.n * A.group - pair0);
         const int tok0 = pair0 / A.group, tok1 = (pair0 + pairs - 1) / A.group;
         const int pos0 = s.kv - s.n + tok0, pos1 = s.kv - s.n + tok1;
         if (pos0 < 0 && split == 0) kv8_report(P, H1B_ERR_INVALID_ARG);
         const Kv8Span span = kv8_span(P, A, pos0, pos1);
         // the tile's blocks in parts of `per`, a multiple of four (one per warp) and at least two per warp
-        const int per = max((((span.count + A.splits - 1) / A.splits) + 3) & ~3, 2 * kRowsWarps);
+        const int per = extra ? span.count + 1 : max((((span.count + splits - 1) / splits) + 3) & ~3, 2 * kRowsWarps);
         const int parts = max(1, (span.count + per - 1) / per);
         if (split >= parts && (parts == 1 || !A.cluster)) continue;
         const int j0 = min(split * per, span.count), j1 = min(j0 + per, span.count);
@@ -622,7 +624,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_ker
                 *reinterpret_cast<float2 *>(res + row * D + ch) = make_float2(a0, a1);
                 if (ch == 0) res_lse[row] = lse2;
             } else {
-                const int64_t part = (((int64_t)idx * P.hkv + kvh) * R + row) * A.splits + split;
+                const int64_t part = (((int64_t)blockIdx.x * P.hkv + kvh) * R + row) * A.splits + split;
                 *reinterpret_cast<float2 *>(A.part_acc + part * D + ch) = make_float2(a0, a1);
                 if (ch == 0) A.part_lse[part] = lse2;
             }
@@ -661,24 +663,34 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_ker
     }
 }
 
-// Joins the parts of the rows whose tokens were dealt into more than one: out = sum_s 2^(lse_s - lse) out_s. A block takes
-// eight pairs of a tile, a warp two of them.
-template <int D>
+// Joins the parts of the rows whose tokens were dealt into more than one: out = sum_s 2^(lse_s - lse) out_s. Up to eight
+// parts: a warp for two rows of a tile. WIDE, more parts (then there are few rows): a block for each row, whose four warps
+// take the parts in turn (one sequence of 16k tokens, 64 parts: 33 -> 19 us; but 13 us more for 8192 rows of two parts).
+// DIRECT: the blocks of the few-rows kernel (a number of tiles for each sequence), else those of the tiles kernel.
+template <int D, bool DIRECT, bool WIDE>
 __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Params P, const Kv8Attn A, const int R, const int unit_blocks,
                                                        const int min_blocks) {
+    __shared__ float sums[4][D + 1];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int idx = blockIdx.x / P.hkv, kvh = blockIdx.x % P.hkv;
     grid_dependency_wait();                                      // launched while the attention kernel's last blocks run
     Kv8Seq s;
     int tile;
-    if (!kv8_find_tile(P, A, idx, R, lane, &s, &tile)) return;
+    if (DIRECT) {
+        s = kv8_seq(P, idx / A.tiles);
+        tile = idx % A.tiles;
+        if (s.n * A.group < A.min_pairs || s.n * A.group > A.max_pairs || tile * R >= s.n * A.group) return;
+    } else if (!kv8_find_tile(P, A, idx, R, lane, &s, &tile)) {
+        return;
+    }
     // the same split of the same tile as the attention kernel's
     const int pair0 = tile * R, pairs = min(R, s.n * A.group - pair0);
     const Kv8Span span = kv8_span(P, A, s.kv - s.n + pair0 / A.group, s.kv - s.n + (pair0 + pairs - 1) / A.group);
     const int per = max(((span.count + A.splits - 1) / A.splits + unit_blocks - 1) / unit_blocks * unit_blocks, min_blocks);
     const int parts = max(1, (span.count + per - 1) / per);
     if (parts == 1) return;
-    for (int row = blockIdx.y * 8 + warp; row < min(pairs, (int)blockIdx.y * 8 + 8); row += 4) {
+    const int row0 = WIDE ? blockIdx.y : blockIdx.y * 8 + warp, row1 = WIDE ? row0 + 1 : blockIdx.y * 8 + 8;
+    for (int row = row0; row < min(pairs, row1); row += 4) {
         const int64_t part = (((int64_t)idx * P.hkv + kvh) * R + row) * A.splits;
         const float *pl = A.part_lse + part, *pa = A.part_acc + part * D;
         float top = -INFINITY;
@@ -691,7 +703,7 @@ __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Params P, const 
 #pragma unroll
         for (int x = 0; x < D / 32; ++x) a[x] = 0.f;
 #pragma unroll 4
-        for (int i = 0; i < parts; ++i) {
+        for (int i = WIDE ? warp : 0; i < parts; i += WIDE ? 4 : 1) {
             const float f = pl[i] == -INFINITY ? 0.f : ex2_approx(pl[i] - top);
             sum += f;
 #pragma unroll
@@ -699,6 +711,19 @@ __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Params P, const 
                 const float2 v = *reinterpret_cast<const float2 *>(pa + (int64_t)i * D + x * 64 + lane * 2);
                 a[2 * x] += f * v.x;
                 a[2 * x + 1] += f * v.y;
+            }
+        }
+        if (WIDE) {
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x) sums[warp][(x >> 1) * 64 + lane * 2 + (x & 1)] = a[x];
+            if (lane == 0) sums[warp][D] = sum;
+            __syncthreads();
+            if (warp != 0) return;
+            sum = sums[0][D] + sums[1][D] + sums[2][D] + sums[3][D];
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x) {
+                const int ch = (x >> 1) * 64 + lane * 2 + (x & 1);
+                a[x] = sums[0][ch] + sums[1][ch] + sums[2][ch] + sums[3][ch];
             }
         }
         const bool empty = top == -INFINITY && !nan;
@@ -714,7 +739,7 @@ __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Params P, const 
 }
 
 template <int D, int FMT, int NB, bool SPLIT>
-cudaError_t launch_rows_of(const Kv8Params &P, const Kv8Attn &A, int grid_tiles, cudaStream_t st) {
+cudaError_t launch_rows_of(const Kv8Params &P, const Kv8Attn &A, cudaStream_t st) {
     constexpr int bytes = rows_smem_bytes<D, NB>();
     static Kv8Once once;
     const cudaError_t e = once.shared_memory(reinterpret_cast<const void *>(kv8_rows_kernel<D, FMT, NB, SPLIT>), bytes);
@@ -725,7 +750,7 @@ cudaError_t launch_rows_of(const Kv8Params &P, const Kv8Attn &A, int grid_tiles,
     attr.val.clusterDim.y = 1;
     attr.val.clusterDim.z = (unsigned)A.splits;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid_tiles, (unsigned)P.hkv, (unsigned)A.splits);
+    cfg.gridDim = dim3((unsigned)P.n_seqs * (unsigned)A.tiles, (unsigned)P.hkv, (unsigned)A.splits);
     cfg.blockDim = dim3(kRowsWarps * 32);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = st;
@@ -745,12 +770,11 @@ cudaError_t launch_kv8_read(const Kv8Params &P, const h1b_kv8_rows &k, const h1b
     return launch_io<false>(P, k, v, d, fmt, bf16, st);
 }
 
-cudaError_t launch_kv8_rows(const Kv8Params &P, const Kv8Attn &A, int d, int fmt, int rows_per_tile, int grid_tiles,
-                            cudaStream_t st) {
+cudaError_t launch_kv8_rows(const Kv8Params &P, const Kv8Attn &A, int d, int fmt, int rows_per_tile, cudaStream_t st) {
     cudaError_t e;
 #define H1B_KV8_ROWS(D, F)                                                                                        \
-    e = rows_per_tile == 8 ? (A.bf16 ? launch_rows_of<D, F, 1, false> : launch_rows_of<D, F, 1, true>)(P, A, grid_tiles, st) \
-                           : (A.bf16 ? launch_rows_of<D, F, 2, false> : launch_rows_of<D, F, 2, true>)(P, A, grid_tiles, st)
+    e = rows_per_tile == 8 ? (A.bf16 ? launch_rows_of<D, F, 1, false> : launch_rows_of<D, F, 1, true>)(P, A, st) \
+                           : (A.bf16 ? launch_rows_of<D, F, 2, false> : launch_rows_of<D, F, 2, true>)(P, A, st)
     if (d == 128 && fmt == H1B_KV8_INT8) { H1B_KV8_ROWS(128, H1B_KV8_INT8); }
     else if (d == 128) { H1B_KV8_ROWS(128, H1B_KV8_E4M3); }
     else if (fmt == H1B_KV8_INT8) { H1B_KV8_ROWS(64, H1B_KV8_INT8); }
@@ -766,13 +790,18 @@ cudaError_t launch_kv8_join(const Kv8Params &P, const Kv8Attn &A, int d, int row
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)A.tiles * (unsigned)P.hkv, (unsigned)(rows_per_tile / 8));
+    const bool direct = rows_per_tile <= 16, wide = direct && A.splits > 8;
+    cfg.gridDim = dim3((unsigned)A.tiles * (direct ? (unsigned)P.n_seqs : 1u) * (unsigned)P.hkv, (unsigned)(wide ? rows_per_tile : rows_per_tile / 8));
     cfg.blockDim = dim3(128);
     cfg.stream = st;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return d == 128 ? cudaLaunchKernelEx(&cfg, kv8_join_kernel<128>, P, A, rows_per_tile, unit_blocks, min_blocks)
-                    : cudaLaunchKernelEx(&cfg, kv8_join_kernel<64>, P, A, rows_per_tile, unit_blocks, min_blocks);
+    auto pick = [&](auto head_dim) {
+        constexpr int D = decltype(head_dim)::value;
+        return !direct ? kv8_join_kernel<D, false, false> : wide ? kv8_join_kernel<D, true, true> : kv8_join_kernel<D, true, false>;
+    };
+    return cudaLaunchKernelEx(&cfg, d == 128 ? pick(std::integral_constant<int, 128>()) : pick(std::integral_constant<int, 64>()),
+                              P, A, rows_per_tile, unit_blocks, min_blocks);
 }
 
 }  // namespace h1b

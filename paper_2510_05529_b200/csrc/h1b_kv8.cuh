@@ -36,7 +36,7 @@ struct Kv8Attn {
     float scale_log2;                      // scale * log2(e)
     int window, sinks;
     int splits;                            // most parts a tile's tokens are dealt into
-    int tiles;                             // no batch of n_rows rows has more tiles than this
+    int tiles;                             // few rows: tiles of a sequence that have a block each; many: the most tiles there are
     int min_pairs;                         // sequences with fewer (row, head of the group) pairs are another kernel's ...
     int max_pairs;                         // ... and those with more
     int cluster;                           // few rows: the parts of a tile are a cluster and join by themselves
@@ -72,21 +72,27 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8Params &P, int i) {
     return s;
 }
 
-// Whole warp: the sequence that row r belongs to; false if it is nobody's.
+__device__ __forceinline__ Kv8Seq kv8_seq_from_lane(const Kv8Seq &s, int b, int src) {
+    return {b, __shfl_sync(~0u, s.start, src), __shfl_sync(~0u, s.n, src), __shfl_sync(~0u, s.kv, src)};
+}
+
+// Whole warp: the sequence that row r belongs to; false if it is nobody's. row_start is searched 32 entries at a time.
 __device__ __forceinline__ bool kv8_seq_of_row(const Kv8Params &P, int r, int lane, Kv8Seq *out) {
-    for (int base = 0; base < P.n_seqs; base += 32) {
-        const Kv8Seq s = kv8_seq(P, base + lane);
-        const unsigned hit = __ballot_sync(~0u, r >= s.start && r < s.start + s.n);
-        if (hit) {
-            const int src = __ffs(hit) - 1;
-            out->b = base + src;
-            out->start = __shfl_sync(~0u, s.start, src);
-            out->n = __shfl_sync(~0u, s.n, src);
-            out->kv = __shfl_sync(~0u, s.kv, src);
-            return true;
-        }
+    int base = 0, count = P.n_seqs;
+    while (count > 32) {
+        const int step = (count + 31) / 32, i = base + lane * step;
+        const int below = __popc(__ballot_sync(~0u, i < base + count && P.row_start[min(i, P.n_seqs)] <= r));
+        if (below == 0) return false;
+        const int next = base + (below - 1) * step;
+        count = min(step, base + count - next);
+        base = next;
     }
-    return false;
+    const Kv8Seq s = kv8_seq(P, lane < count ? base + lane : P.n_seqs);
+    const unsigned hit = __ballot_sync(~0u, r >= s.start && r < s.start + s.n);
+    if (!hit) return false;
+    const int src = __ffs(hit) - 1;
+    *out = kv8_seq_from_lane(s, base + src, src);
+    return true;
 }
 
 // Whole warp: tile `idx` of the batch. The (row, head of the group) pairs of a sequence, pair = row * group + head, are cut
@@ -107,10 +113,7 @@ __device__ __forceinline__ bool kv8_find_tile(const Kv8Params &P, const Kv8Attn 
         const unsigned hit = __ballot_sync(~0u, idx - before < upto);
         if (hit) {
             const int src = __ffs(hit) - 1;
-            out->b = base + src;
-            out->start = __shfl_sync(~0u, s.start, src);
-            out->n = __shfl_sync(~0u, s.n, src);
-            out->kv = __shfl_sync(~0u, s.kv, src);
+            *out = kv8_seq_from_lane(s, base + src, src);
             *tile = idx - before - __shfl_sync(~0u, upto - own, src);
             return true;
         }
@@ -239,12 +242,22 @@ cudaError_t launch_kv8_append(const Kv8Params &P, const h1b_kv8_rows &k, const h
                               cudaStream_t st);
 cudaError_t launch_kv8_read(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_rows &v, int d, int fmt, int bf16,
                             cudaStream_t st);
-cudaError_t launch_kv8_rows(const Kv8Params &P, const Kv8Attn &A, int d, int fmt, int rows_per_tile, int grid_tiles,
-                            cudaStream_t st);
+cudaError_t launch_kv8_rows(const Kv8Params &P, const Kv8Attn &A, int d, int fmt, int rows_per_tile, cudaStream_t st);
 
 cudaError_t launch_kv8_tiles(const Kv8Params &P, const Kv8Attn &A, int d, int fmt, cudaStream_t st);
 cudaError_t launch_kv8_join(const Kv8Params &P, const Kv8Attn &A, int d, int rows_per_tile, int unit_blocks, int min_blocks,
                             cudaStream_t st);
+
+// A launch whose error is its own (and not one that somebody left behind).
+template <class Kernel, class... Args>
+cudaError_t kv8_launch(Kernel kernel, dim3 grid, int threads, int smem, cudaStream_t st, const Args &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
 
 int report_error(int code, const char *fmt, ...);      // h1b_api.cu: the text behind h1b_last_error(NULL)
 

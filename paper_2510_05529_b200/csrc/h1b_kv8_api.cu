@@ -46,7 +46,7 @@ int check_pool(const h1b_kv8_pool *p) {
 
 int check_batch(const h1b_kv8_pool *p, const h1b_kv8_batch *b) {
     if (!b) return report_error(H1B_ERR_NULL, "batch is NULL");
-    if (b->n_seqs < 0 || b->n_rows < 0 || b->table_width < 1)
+    if (b->n_seqs < 0 || b->n_seqs > 1 << 20 || b->n_rows < 0 || b->table_width < 1)
         return report_error(H1B_ERR_INVALID_ARG, "n_seqs = %d, n_rows = %d, table_width = %d out of range", b->n_seqs,
                             b->n_rows, b->table_width);
     if ((int64_t)b->table_width * p->page_tokens > (1 << 30))
@@ -102,7 +102,10 @@ Kv8Params params_of(const h1b_kv8_pool *p, const h1b_kv8_batch *b) {
 #define H1B_KV8_TRY(expr)                                                                                        \
     do {                                                                                                         \
         const cudaError_t e_ = (expr);                                                                           \
-        if (e_ != cudaSuccess) return report_error(H1B_ERR_CUDA, "%s: %s", #expr, cudaGetErrorString(e_));       \
+        if (e_ != cudaSuccess) {                                                                                 \
+            (void)cudaGetLastError(); /* reported here, and not left for somebody else to find */                \
+            return report_error(H1B_ERR_CUDA, "%s: %s", #expr, cudaGetErrorString(e_));                          \
+        }                                                                                                        \
     } while (0)
 
 int check_io(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8_rows *k, const h1b_kv8_rows *v, int dtype,
@@ -119,12 +122,14 @@ int check_io(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b_kv8
 
 // How the attention of a batch is launched; a function of sizes only. Sequences with at most kFewPairs (row, head of the
 // group) pairs go to the kernel for few rows, the others to the tensor-core tiles; both are launched only when the host
-// cannot tell that one of them has nothing to do.
+// cannot tell that one of them has nothing to do. The border, in us, few rows / tiles (32 / 8 heads of 128): 8 sequences of
+// 8k tokens, 32 pairs: 97 / 109, 48 pairs: 127 / 109; one of 16k tokens: 35 / 49, 41 / 49, 64 pairs: 47 / 50; 32 sequences of
+// 2k tokens: 104 / 94, 124 / 95.
 constexpr int kFewPairs = 32;
 
 struct AttnPart {
     bool used = false, cluster = false;
-    int rows_per_tile = 0, tiles = 0, grid_tiles = 0, splits = 1, min_pairs = 1, max_pairs = 1 << 30;
+    int rows_per_tile = 0, tiles = 0, splits = 1, min_pairs = 1, max_pairs = 1 << 30;
     size_t lines = 0;                                            // partial results
 };
 struct AttnPlan {
@@ -146,18 +151,17 @@ AttnPlan plan_of(const h1b_kv8_pool *p, const h1b_kv8_batch *b, int hq, int wind
         if (a.many.used) f.max_pairs = kFewPairs;
         const int64_t here = std::min<int64_t>(most, f.max_pairs);
         f.rows_per_tile = here <= 8 ? 8 : 16;
-        const int64_t hinted = (int64_t)b->n_seqs * ((here + f.rows_per_tile - 1) / f.rows_per_tile);
-        f.tiles = (int)(pairs / f.rows_per_tile + seqs);
-        if (a.many.used) f.tiles = (int)std::min<int64_t>(f.tiles, hinted);    // (no sequence has more)
-        f.grid_tiles = (int)std::min<int64_t>(f.tiles, hinted);
+        f.tiles = (int)((here + f.rows_per_tile - 1) / f.rows_per_tile);       // of a sequence
         // Parts. The GPU holds 148 * 4 blocks of 8-row tiles at once (half as many of 16 rows). Fill it once, as far as there
-        // are 128 tokens for each block (two blocks of 16 a warp); go to four times as many blocks, so that ragged lengths
-        // even out, where each still has 1024 tokens (more and shorter ones cost: 32 sequences with a window of 1024 tokens
-        // took 24 us in seven parts and 16 in two). The last limit bounds the workspace when max_rows says far less than the
-        // batch holds.
-        const int64_t blocks = (int64_t)f.grid_tiles * p->n_kv_heads, slots = f.rows_per_tile == 8 ? 148 * 4 : 148 * 2;
-        const int64_t fill = std::min<int64_t>(slots / blocks, (seen + 127) / 128), even = std::min<int64_t>(4 * slots / blocks, seen / 1024);
-        f.splits = (int)std::max<int64_t>(1, std::min<int64_t>({std::max(fill, even), 256, 148 * 48 / ((int64_t)f.tiles * p->n_kv_heads)}));
+        // are 128 tokens for each block (two blocks of 16 a warp); fill it up to four times, so that ragged lengths even out,
+        // where each block still has 1024 tokens (more and shorter ones cost: 32 sequences with a window of 1024 tokens took
+        // 24 us in seven parts and 15 in two).
+        const int64_t blocks = (int64_t)b->n_seqs * f.tiles * p->n_kv_heads, slots = f.rows_per_tile == 8 ? 148 * 4 : 148 * 2;
+        const int64_t fill = std::min<int64_t>(slots / blocks, (seen + 127) / 128);
+        int64_t even = 0;
+        for (int64_t times = 4; times >= 1 && !even; --times)
+            if (times * slots / blocks <= seen / 1024) even = times * slots / blocks;
+        f.splits = (int)std::max<int64_t>(1, std::min<int64_t>(std::max(fill, even), 256));
         // Up to eight parts (the largest cluster that every GPU takes) join through each other's shared memory, others through
         // the workspace and a kernel of its own, some 2 us more (one sequence of 777 tokens: 6.7 and 8.6 us). Blocks that come
         // in several waves do better without clusters, whose parts start and end together (16 sequences of 4-8k tokens, 32
@@ -168,7 +172,7 @@ AttnPlan plan_of(const h1b_kv8_pool *p, const h1b_kv8_batch *b, int hq, int wind
         AttnPart &m = a.many;
         if (a.few.used) m.min_pairs = kFewPairs + 1;
         m.rows_per_tile = 256;
-        m.tiles = m.grid_tiles = (int)(pairs / 256 + seqs);
+        m.tiles = (int)(pairs / 256 + std::min<int64_t>(seqs, pairs / m.min_pairs));
         // Parts only where there are too few tiles for the SMs (one block an SM): up to three times as many blocks as SMs, so
         // that ragged lengths even out, each of at least 512 tokens (six sequences with 5 to 131 rows over 1-9k tokens: 206 us
         // at one block an SM, 172, 163 and 163 at two, three and four, 180 at six).
@@ -177,7 +181,7 @@ AttnPlan plan_of(const h1b_kv8_pool *p, const h1b_kv8_batch *b, int hq, int wind
     }
     for (AttnPart *part : {&a.few, &a.many})
         if (part->used && part->splits > 1 && !part->cluster) {
-            part->lines = (size_t)part->tiles * p->n_kv_heads * part->rows_per_tile * part->splits;
+            part->lines = (size_t)part->tiles * (part == &a.few ? b->n_seqs : 1) * p->n_kv_heads * part->rows_per_tile * part->splits;
             a.bytes += part->lines * (p->head_dim + 1) * sizeof(float);
         }
     return a;
@@ -272,7 +276,7 @@ int h1b_kv8_attention(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, cons
     }
     if (plan.few.used) {
         take(plan.few);
-        H1B_KV8_TRY(launch_kv8_rows(P, A, pool->head_dim, pool->format, plan.few.rows_per_tile, plan.few.grid_tiles, st));
+        H1B_KV8_TRY(launch_kv8_rows(P, A, pool->head_dim, pool->format, plan.few.rows_per_tile, st));
     }
     return H1B_OK;
 }

@@ -702,8 +702,7 @@ cudaError_t launch_of(const Kv8Params &P, const Kv8Attn &A, cudaStream_t st) {
     const cudaError_t e = once.shared_memory(reinterpret_cast<const void *>(kv8_tiles_kernel<D, FMT, SPLIT>), bytes);
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)A.tiles * (unsigned)P.hkv, 1, (unsigned)A.splits);
-    kv8_tiles_kernel<D, FMT, SPLIT><<<grid, kTlThreads, bytes, st>>>(P, A);
-    return cudaGetLastError();
+    return kv8_launch(kv8_tiles_kernel<D, FMT, SPLIT>, grid, kTlThreads, bytes, st, P, A);
 }
 
 }  // namespace

@@ -208,6 +208,28 @@ def test_random_batches(binding):
         check_attention(got, lse, want, tag=str(case))
 
 
+@pytest.mark.parametrize("seqs", [33, 70, 1100])
+def test_many_sequences(binding, seqs):
+    """More sequences than a warp has lanes, empty ones among them, single rows and chunks in one batch."""
+    rng = np.random.default_rng(seqs)
+    rows = [int(x) for x in rng.choice([0, 1, 1, 1, 2, 5], seqs)]
+    rows[-1] = 1
+    if seqs < 100:
+        rows[3], rows[-2] = 90, 300
+    kv = [r + int(rng.integers(0, 60)) for r in rows]
+    got, lse, want = run_case(binding, (rows, kv, 4, 2, 64, 16, "int8", BF16, 0, 0), seed=3)
+    check_attention(got, lse, want)
+    b = Batch(rows, kv, 16, seed=1)
+    pages = pages_of(binding, empty_pool(b.n_pages, 2, 16, 64, "int8"))
+    k, v = (torch.randn(b.n_rows, 2, 64).to(F16) for _ in "kv")
+    args = b.tensors()
+    pages.h1b_kv8_append(k.cuda(), v.cuda(), *args)
+    for x, y in zip((k, v), pages.h1b_kv8_read(*args, n_rows=b.n_rows)):
+        q, sc = quantised(x, "int8")
+        assert torch.equal(y.cpu(), (q.float() * sc.float()[..., None]).to(F16))
+    pages.h1b_kv8_poll_status()
+
+
 def test_rows_that_see_nothing(binding):
     """kv_len smaller than the rows: the first rows lie before the sequence and get zeros; the status says so."""
     for hq, n in ((2, 3), (8, 200)):

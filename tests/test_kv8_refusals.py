@@ -47,7 +47,7 @@ BAD_POOLS = [
     (dict(k=None), -2), (dict(v=None), -2), (dict(k_scale=None), -2), (dict(v_scale=None), -2), (dict(k=P + 8), -1), (dict(v_scale=P + 4), -1),
 ]
 BAD_BATCHES = [
-    (dict(n_seqs=-1), -1), (dict(n_rows=-1), -1), (dict(table_width=0), -1), (dict(table_width=1 << 26), -1), (dict(block_table=None), -2),
+    (dict(n_seqs=-1), -1), (dict(n_seqs=2 ** 20 + 1), -1), (dict(n_rows=-1), -1), (dict(table_width=0), -1), (dict(table_width=1 << 26), -1), (dict(block_table=None), -2),
     (dict(kv_len=None), -2), (dict(row_start=None), -2),
 ]
 BAD_IN = [(dict(data=None), -2), (dict(data=P + 2), -1), (dict(row_stride=12), -1), (dict(head_stride=4), -1)]
