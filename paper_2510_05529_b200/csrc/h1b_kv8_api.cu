@@ -143,9 +143,12 @@ AttnPlan plan_of(const h1b_kv8_pool *p, const h1b_kv8_batch *b, int hq, int wind
     const int64_t rows = std::min<int64_t>(std::max(max_rows, 1), b->n_rows), most = rows * group;
     const int64_t seqs = std::min(b->n_seqs, b->n_rows);
     a.many.used = most > kFewPairs;
-    a.few.used = !a.many.used || (b->n_seqs > 1 && rows * b->n_seqs > b->n_rows);
     const int64_t cap = (int64_t)b->table_width * p->page_tokens;
     const int64_t seen = window ? std::min<int64_t>(cap, (int64_t)window + sinks + rows + 32) : cap;
+    // (The kernel for few rows is also left out where the tiles of all sequences together are less work than its launches:
+    // five steps of 64 tokens an SM. Four sequences of 2-132 rows over 175 tokens: 24 us with it, 16 without.)
+    a.few.used = !a.many.used || (b->n_seqs > 1 && rows * b->n_seqs > b->n_rows &&
+                                  (pairs / 256 + seqs) * p->n_kv_heads * seen > 148 * 5 * 64);
     if (a.few.used) {
         AttnPart &f = a.few;
         if (a.many.used) f.max_pairs = kFewPairs;

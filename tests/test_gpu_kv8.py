@@ -145,6 +145,10 @@ CASES = [
     ([140], [2100], 12, 4, 128, 128, "e4m3", BF16, 700, 1),
     ([513], [513], 2, 1, 128, 256, "int8", F16, 1, 1),
     ([129], [4000], 5, 1, 128, 64, "int8", BF16, 0, 0),
+    # enough work for both kernels in one call: single tokens and short rows beside chunks
+    ([1, 2, 40, 150, 8], [6000, 3000, 5000, 4000, 9], 8, 2, 128, 64, "int8", F16, 0, 0),
+    ([150, 1, 0, 3, 70], [4000, 7000, 0, 5000, 70], 6, 2, 64, 32, "e4m3", BF16, 0, 0),
+    ([100, 1, 4], [7000, 7000, 3000], 16, 4, 128, 16, "e4m3", F16, 3000, 9),
 ]
 
 
