@@ -249,7 +249,8 @@ int h1b_kv8_attention(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, cons
     if (rc == H1B_OK) rc = check_rows("out", out, batch->n_rows, n_q_heads, pool->head_dim, true, false);
     if (rc == H1B_OK) rc = check_type(dtype);
     if (rc != H1B_OK) return rc;
-    if (!std::isfinite(scale)) return report_error(H1B_ERR_INVALID_ARG, "scale is not finite");
+    const float scale_log2 = (float)((double)scale * 1.4426950408889634074);
+    if (!std::isfinite(scale_log2)) return report_error(H1B_ERR_INVALID_ARG, "scale or scale * log2(e) is not finite");
     if (batch->n_rows == 0 || batch->n_seqs == 0) return H1B_OK;
     const AttnPlan plan = plan_of(pool, batch, n_q_heads, window, sinks, max_rows);
     if (plan.bytes && (!workspace || workspace_bytes < plan.bytes || !aligned16(workspace)))
@@ -261,7 +262,7 @@ int h1b_kv8_attention(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, cons
     A.q = q->data; A.out = out->data; A.lse = lse;
     A.q_rs = q->row_stride; A.q_hs = q->head_stride; A.o_rs = out->row_stride; A.o_hs = out->head_stride;
     A.hq = n_q_heads; A.group = n_q_heads / pool->n_kv_heads; A.bf16 = dtype == H1B_TYPE_BF16;
-    A.scale_log2 = (float)((double)scale * 1.4426950408889634074);
+    A.scale_log2 = scale_log2;
     A.window = window; A.sinks = window ? sinks : 0;
     const Kv8Params P = params_of(pool, batch);
     float *at = static_cast<float *>(workspace);

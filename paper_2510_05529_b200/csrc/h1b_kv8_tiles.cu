@@ -1,23 +1,30 @@
 // 8-bit pages: attention for many rows per sequence (prompts and chunks of them) on the 5th-generation tensor cores.
 //
-// One block of 19 warps takes 256 (row, head of the group) pairs of a sequence that share a KV head, as two tiles of 128
-// pairs, and one part of the tokens they see, 64 tokens at a time (four blocks of 16, whichever blocks the span lists: sinks
-// and window need not be neighbours). The roles hand each other operands through mbarriers; nothing in the loop is
-// block-wide:
-//   warps 8-15   convert (four warps the keys, four the values): codes come from the pages in 16-byte copies, two
+// One block of 27 warps (and one that only hands over its registers) takes 256 (row, head of the group) pairs of a sequence
+// that share a KV head, as two tiles of 128 pairs, and one part of the tokens they see, 64 tokens at a time (four blocks of
+// 16, whichever blocks the span lists: sinks and window need not be neighbours). The roles hand each other operands through
+// mbarriers; nothing in the loop is block-wide:
+//   warps 0-7    softmax of tile A, warps 8-15 of tile B, 16 rows a warp: scores S * ks * qs, the rows' references,
+//                weights w = 2^(score - m) * vs / sigma in fp16, written over the scores they came from;
+//   warps 16-23  convert (four warps the keys, four the values): codes come from the pages in 16-byte copies, two
 //                steps ahead, become exact fp16 numbers ONCE for all 256 pairs and go to shared memory as matrix
 //                operands (three of each, 128-byte swizzle; keys K-major, values with the channels contiguous, so nothing
 //                is transposed);
-//   warp 18      brings the tokens' scales;
-//   warps 16, 17 issue the contractions of tile A and of tile B: S = Q K^T into tensor memory, O += P V with P read from
+//   warps 24, 25 issue the contractions of tile A and of tile B: S = Q K^T into tensor memory, O += P V with P read from
 //                tensor memory;
-//   warps 0-3    softmax of tile A, warps 4-7 of tile B, 32 rows a warp: scores S * ks * qs, the rows' references,
-//                weights w = 2^(score - m) * vs / sigma in fp16, written over the scores they came from.
+//   warp 26      brings the tokens' scales and says what of a step needs masks.
 // Tensor memory holds two sets of scores for each tile, so the scores of the next step are there when a softmax warp has
-// finished with this one: with one set of 128 columns a step took softmax and contractions one after the other (7400
-// cycles for 128 tokens instead of the longer of the two). m and sigma follow lazily (as in the kernel for few rows): O is
-// rescaled only when a score exceeds m by 4 (in log2) or a value scale exceeds 4 sigma; weights are carried times 2^9. For
-// fp16 results (SPLIT) a second contraction adds what rounding the weights left over.
+// finished with this one. m and sigma follow lazily (as in the kernel for few rows): O is rescaled only when a score exceeds
+// m by 4 (in log2) or a value scale exceeds 4 sigma; weights are carried times 2^9. For fp16 results (SPLIT) a second
+// contraction adds what rounding the weights left over.
+//
+// What bounds it: instruction issue (66 % of the slots; the tensor cores are busy 40 % of the time). A prompt of 8192 tokens,
+// 32 heads of 128, takes 825 us = 668 TFLOP/s, 40 % of the measured bf16 rate; a softmax warp spends some 290 instructions on
+// a step, half of them the arithmetic of its 16 x 64 scores. Steps on the way there (the same prompt): one thread issuing
+// for both tiles, a single set of scores and 128 tokens a step 1194 us (the roles' loops together did not fit the instruction
+// cache: 85 % hits), two threads, two sets, 64 tokens 935 (99 % hits), copies two steps ahead and a warp for the scales 873,
+// sixteen softmax warps of 16 rows instead of eight of 32 (more warps to hide each other's latencies) 841, the masks' flags
+// made by the scales' warp 825.
 // Every wait is bounded; a role that gives up records the time-out and leaves, and the block releases its tensor memory.
 #include <type_traits>
 
@@ -28,10 +35,9 @@ namespace h1b {
 namespace {
 
 constexpr int kTlRows = 128, kTlKeys = 64, kTlBlocks = kTlKeys / kKv8Block;
-constexpr int kTlHalves = 1;                                   // 16-row fragments a softmax warp has
-constexpr int kTlSoftmax = 16 / kTlHalves;                     // warps 0 .. softmax, then 8 convert, 2 issue, 1 scales;
-constexpr int kTlThreads = (kTlSoftmax + 12) * 32;             // the last only hands over its registers
-constexpr int kTlRegsLaunch = kTlHalves == 1 ? 72 : 96, kTlRegsSoftmax = kTlHalves == 1 ? 88 : 152, kTlRegsConvert = 48, kTlRegsIssue = 56;
+constexpr int kTlSoftmax = 16;                                 // softmax warps, then 8 convert, 2 issue, 1 scales; the last
+constexpr int kTlThreads = (kTlSoftmax + 12) * 32;             // only hands over its registers
+constexpr int kTlRegsLaunch = 72, kTlRegsSoftmax = 88, kTlRegsConvert = 48, kTlRegsIssue = 56;
 static_assert(kTlSoftmax * 32 * kTlRegsSoftmax + 256 * kTlRegsConvert + 128 * kTlRegsIssue <= kTlThreads * kTlRegsLaunch,
               "more registers than a block is launched with");
 constexpr float kTlLazy = 4.f, kTlWeightUnit = 512.f;
@@ -203,11 +209,10 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
     if (warp < kTlSoftmax) {
         more_registers<kTlRegsSoftmax>();
         // ---------------------------------------------------------------------------------------- softmax
-        // A warp has 32 rows of a tile in fragment layout: rows gi + 8 q (q = 0 .. 3) of them are this lane's, four lanes to a
-        // row. (A warp reaches the quarter of tensor memory of its number % 4.)
+        // A warp has 16 rows of a tile in fragment layout: rows gi and gi + 8 of them are this lane's, four lanes to a row.
+        // (A warp reaches the quarter of tensor memory of its number % 4.)
         const int qt = warp / (kTlSoftmax / 2), gi = lane >> 2, tj = lane & 3;
-        const int row0 = (warp & 3) * 32 + (kTlHalves == 1 ? (warp & 4) * 4 : 0);
-        constexpr int NQ = 2 * kTlHalves;
+        const int row0 = (warp & 3) * 32 + (warp & 4) * 4;
         // the query rows, two threads to a row: fp16 multiplied by 2^-e, negated if the scale is negative, into the K-major
         // operand
 #pragma unroll 1
@@ -257,9 +262,9 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
 
         const uint32_t t_lane = W.tmem + ((uint32_t)row0 << 16), t_o = t_lane + 4 * kTlKeys + qt * D;
         const int n_tiles = W.n_tiles;
-        uint64_t qs2[NQ], nm2[NQ], l2[NQ];                          // of each row, twice: qs, -m, and the two halves of the sum
+        uint64_t qs2[2], nm2[2], l2[2];                              // of each row, twice: qs, -m, and the two halves of the sum
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
+        for (int q = 0; q < 2; ++q) {
             const float qs = reinterpret_cast<const float *>(smem + M::kRows)[qt * kTlRows + row0 + 8 * q + gi];
             qs2[q] = pack2f(qs, qs);
             nm2[q] = pack2f(INFINITY, INFINITY);
@@ -274,24 +279,22 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                 }
                 tc_fence_after_sync();
                 const uint32_t t_s = t_lane + (qt * 2 + (i & 1)) * kTlKeys;
-                uint32_t sv[2][kTlHalves][16];                            // [32 columns][16 rows]
+                uint32_t sv[2][16];                              // [32 columns]
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int h = 0; h < kTlHalves; ++h) tmem_ld_frag_issue(t_s + c * 32 + ((uint32_t)(16 * h) << 16), sv[c][h]);
+                for (int c = 0; c < 2; ++c) tmem_ld_frag_issue(t_s + c * 32, sv[c]);
                 const unsigned char *stage = smem + M::kScales + (i & 3) * M::kStage;
                 const unsigned char *ks = stage + tj * 8, *vs = ks + M::kVs;   // pairs of columns 8 b + 2 tj, + 1
                 const int *first = reinterpret_cast<const int *>(stage + M::kFirst);
                 const int how = first[6 + qt];
                 const bool whole = how & 1;
                 // bit 2 b + x of seen[q]: row q of the lane sees column 8 b + 2 tj + x
-                uint32_t seen[NQ] = {};
+                uint32_t seen[2] = {};
                 if (!whole) {
 #pragma unroll 1
                     for (int b = 7; b >= 0; --b) {
                         const int t = first[b >> 1] + (b & 1) * 8 + 2 * tj;
 #pragma unroll
-                        for (int q = 0; q < NQ; ++q) {
+                        for (int q = 0; q < 2; ++q) {
                             const int pos = row_pos[8 * q];
                             const bool s0 = t <= pos && (!A.window || t > pos - A.window || t < A.sinks);
                             const bool s1 = t + 1 <= pos && (!A.window || t + 1 > pos - A.window || t + 1 < A.sinks);
@@ -301,19 +304,17 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                 }
                 tmem_ld_wait();
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int h = 0; h < kTlHalves; ++h) tmem_tie16(sv[c][h]);
+                for (int c = 0; c < 2; ++c) tmem_tie16(sv[c]);
                 // ---- scores times the keys' scales, and the rows' largest (before qs >= 0) ----
-                float top[NQ];
+                float top[2];
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) top[q] = -INFINITY;
+                for (int q = 0; q < 2; ++q) top[q] = -INFINITY;
 #pragma unroll
                 for (int b = 0; b < 8; ++b) {
                     const uint64_t kk = *reinterpret_cast<const uint64_t *>(ks + b * 32);
 #pragma unroll
-                    for (int q = 0; q < NQ; ++q) {
-                        uint32_t *r = &sv[b >> 2][q >> 1][(b & 3) * 4 + (q & 1) * 2];
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t *r = &sv[b >> 2][(b & 3) * 4 + q * 2];
                         const float2 z = unpack2(mul2(pack2(r[0], r[1]), kk));
                         r[0] = __float_as_uint(z.x);
                         r[1] = __float_as_uint(z.y);
@@ -323,26 +324,26 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
 #pragma unroll
                     for (int b = 0; b < 8; ++b)
 #pragma unroll
-                        for (int q = 0; q < NQ; ++q)
+                        for (int q = 0; q < 2; ++q)
 #pragma unroll
                             for (int x = 0; x < 2; ++x)
-                                if (!(seen[q] >> (2 * b + x) & 1)) sv[b >> 2][q >> 1][(b & 3) * 4 + (q & 1) * 2 + x] = 0xFF800000u;
+                                if (!(seen[q] >> (2 * b + x) & 1)) sv[b >> 2][(b & 3) * 4 + q * 2 + x] = 0xFF800000u;
                 }
 #pragma unroll
                 for (int b = 0; b < 8; ++b)
 #pragma unroll
-                    for (int q = 0; q < NQ; ++q) {
-                        const uint32_t *r = &sv[b >> 2][q >> 1][(b & 3) * 4 + (q & 1) * 2];
+                    for (int q = 0; q < 2; ++q) {
+                        const uint32_t *r = &sv[b >> 2][(b & 3) * 4 + q * 2];
                         top[q] = max3(top[q], __uint_as_float(r[0]), __uint_as_float(r[1]));
                     }
                 float over = -INFINITY;                           // how far a score lies above its row's reference
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) over = fmaxf(over, fmaf(top[q], unpack2(qs2[q]).x, unpack2(nm2[q]).x));
+                for (int q = 0; q < 2; ++q) over = fmaxf(over, fmaf(top[q], unpack2(qs2[q]).x, unpack2(nm2[q]).x));
                 if (__any_sync(~0u, over > kTlLazy) || (how & 2)) {
                     const float turn = reinterpret_cast<const float *>(first)[4];
-                    float f[NQ];
+                    float f[2];
 #pragma unroll
-                    for (int q = 0; q < NQ; ++q) {
+                    for (int q = 0; q < 2; ++q) {
                         const float m = -unpack2(nm2[q]).x;
                         float x = top[q] == -INFINITY ? top[q] : top[q] * unpack2(qs2[q]).x;
                         x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
@@ -358,19 +359,16 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                         // one with the same barrier is long done: the scores of step i - 1 were issued after it)
                         if (!warp_wait(bar(kBarPV + qt * 2 + ((i - 1) & 1)), ((i - 1) >> 1) & 1)) { failed = true; break; }
                         tc_fence_after_sync();
-#pragma unroll
-                        for (int h = 0; h < kTlHalves; ++h)
 #pragma unroll 1
-                            for (int c = 0; c < D; c += 32) {
-                                const uint32_t at = t_o + c + ((uint32_t)(16 * h) << 16);
-                                uint32_t ov[16];
-                                tmem_ld_frag_issue(at, ov);
-                                tmem_ld_wait();
-                                tmem_tie16(ov);
+                        for (int c = 0; c < D; c += 32) {
+                            uint32_t ov[16];
+                            tmem_ld_frag_issue(t_o + c, ov);
+                            tmem_ld_wait();
+                            tmem_tie16(ov);
 #pragma unroll
-                                for (int x = 0; x < 16; ++x) ov[x] = __float_as_uint(__uint_as_float(ov[x]) * f[2 * h + ((x >> 1) & 1)]);
-                                tmem_st_frag_f32(at, ov);
-                            }
+                            for (int x = 0; x < 16; ++x) ov[x] = __float_as_uint(__uint_as_float(ov[x]) * f[(x >> 1) & 1]);
+                            tmem_st_frag_f32(t_o + c, ov);
+                        }
                         tmem_st_wait();
                     }
                 }
@@ -379,13 +377,13 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                     constexpr bool MASK = decltype(masked)::value;
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        uint32_t hi[kTlHalves][8], lo[kTlHalves][8];
+                        uint32_t hi[8], lo[8];
 #pragma unroll
                         for (int b = 0; b < 4; ++b) {
                             const uint64_t vv = *reinterpret_cast<const uint64_t *>(vs + (c * 4 + b) * 32);
 #pragma unroll
-                            for (int q = 0; q < NQ; ++q) {
-                                const uint32_t *r = &sv[c][q >> 1][b * 4 + (q & 1) * 2];
+                            for (int q = 0; q < 2; ++q) {
+                                const uint32_t *r = &sv[c][b * 4 + q * 2];
                                 const float2 z = unpack2(fma2(pack2(r[0], r[1]), qs2[q], nm2[q]));
                                 float p0 = ex2_approx(z.x), p1 = ex2_approx(z.y);
                                 const bool s0 = !MASK || (seen[q] >> (8 * c + 2 * b) & 1);
@@ -404,21 +402,17 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                                     ww = pack2f(w.x, w.y);
                                 }
                                 const float2 w = unpack2(ww);
-                                uint32_t &h = hi[q >> 1][b * 2 + (q & 1)];
+                                uint32_t &h = hi[b * 2 + q];
                                 h = pack_f16x2(w.x, w.y);
                                 if (SPLIT) {
                                     const float2 back = half2_bits_to_float2(h);
                                     const float2 rest = unpack2(fma2(pack2f(back.x, back.y), pack2f(-1.f, -1.f), ww));
-                                    lo[q >> 1][b * 2 + (q & 1)] = pack_f16x2(rest.x, rest.y);
+                                    lo[b * 2 + q] = pack_f16x2(rest.x, rest.y);
                                 }
                             }
                         }
-#pragma unroll
-                        for (int h = 0; h < kTlHalves; ++h) {
-                            const uint32_t to = t_s + c * 32 + ((uint32_t)(16 * h) << 16);
-                            if (SPLIT) tmem_st_frag32(to, hi[h], lo[h]);
-                            else tmem_st_frag16(to, hi[h]);
-                        }
+                        if (SPLIT) tmem_st_frag32(t_s + c * 32, hi, lo);
+                        else tmem_st_frag16(t_s + c * 32, hi);
                     }
                 };
                 if (whole) weigh(std::false_type()); else weigh(std::true_type());
@@ -434,12 +428,12 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                 float sigma = 0.f;
                 if (n_tiles > 0) sigma = reinterpret_cast<const float *>(smem + M::kScales + ((n_tiles - 1) & 3) * M::kStage + M::kFirst)[5];
                 const int parts = W.parts;
-                float inv[NQ];
-                bool live[NQ];
-                uint16_t *op[NQ];
-                float *pa[NQ];
+                float inv[2];
+                bool live[2];
+                uint16_t *op[2];
+                float *pa[2];
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) {
+                for (int q = 0; q < 2; ++q) {
                     const float2 x = unpack2(l2[q]);
                     float l = x.x + x.y;
                     l += __shfl_xor_sync(~0u, l, 1);
@@ -458,35 +452,32 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                         else if (A.lse) A.lse[(int64_t)tok * A.hq + head] = lse2 * kLn2;
                     }
                 }
-#pragma unroll
-                for (int h = 0; h < kTlHalves; ++h)
 #pragma unroll 1
-                    for (int c = 0; c < D; c += 32) {
-                        uint32_t ov[16];
-                        if (n_tiles > 0) {
-                            tmem_ld_frag_issue(t_o + c + ((uint32_t)(16 * h) << 16), ov);
-                            tmem_ld_wait();
-                            tmem_tie16(ov);
-                        }
-#pragma unroll
-                        for (int b = 0; b < 4; ++b)
-#pragma unroll
-                            for (int y = 0; y < 2; ++y) {
-                                const int q = 2 * h + y;
-                                if (!live[q]) continue;
-                                const float u = n_tiles > 0 ? __uint_as_float(ov[b * 4 + y * 2]) * inv[q] : 0.f;
-                                const float v = n_tiles > 0 ? __uint_as_float(ov[b * 4 + y * 2 + 1]) * inv[q] : 0.f;
-                                if (parts == 1) *reinterpret_cast<uint32_t *>(op[q] + c + b * 8) = float2_to_pair(u, v, A.bf16);
-                                else *reinterpret_cast<float2 *>(pa[q] + c + b * 8) = make_float2(u, v);
-                            }
-                        __syncwarp();
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t ov[16];
+                    if (n_tiles > 0) {
+                        tmem_ld_frag_issue(t_o + c, ov);
+                        tmem_ld_wait();
+                        tmem_tie16(ov);
                     }
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            if (!live[q]) continue;
+                            const float u = n_tiles > 0 ? __uint_as_float(ov[b * 4 + q * 2]) * inv[q] : 0.f;
+                            const float v = n_tiles > 0 ? __uint_as_float(ov[b * 4 + q * 2 + 1]) * inv[q] : 0.f;
+                            if (parts == 1) *reinterpret_cast<uint32_t *>(op[q] + c + b * 8) = float2_to_pair(u, v, A.bf16);
+                            else *reinterpret_cast<float2 *>(pa[q] + c + b * 8) = make_float2(u, v);
+                        }
+                    __syncwarp();
+                }
             }
         }
     } else if (warp < kTlSoftmax + 8) {
         fewer_registers<kTlRegsConvert>();
         // ---------------------------------------------------------------------------------------- convert
-        const bool keys = warp < kTlSoftmax + 4;                                           // warps 8-11 keys, 12-15 values
+        const bool keys = warp < kTlSoftmax + 4;
         const int cw = warp & 3;
         constexpr int ROWS_IT = D == 128 ? 4 : 8, ITS = 16 / ROWS_IT;          // rows per 512 bytes, loads per thread and step
         // A warp converts one block of each step. lane -> (row, 16 channels) such that eight neighbouring lanes write 128
