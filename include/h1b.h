@@ -541,7 +541,11 @@ int h1b_kv8_read(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b
  *           sum of exp(scale q k) over the tokens seen (for joining the result
  *           with attention over other tokens). A row that sees nothing gets
  *           zeros and lse = -infinity.
- *   scale   finite
+ *   scale   finite (times log2(e) too)
+ *   Sizes: whatever fp16 holds is computed to the precision above. Of bf16's
+ *           range, so are values of any size above 2^-110, query rows whose
+ *           largest number is above 2^-86, and keys below 2^98; a score beyond
+ *           fp32's range is an infinity, and its row then NaN.
  *   max_rows  the largest n_b of the batch as far as the host knows it (1 for a
  *           decode step; n_rows is always right): it chooses kernels and
  *           launch sizes only, every row is computed whatever it says.

@@ -124,6 +124,7 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Io io) {
     };
     uint4 next[2];
     load(h0 * 2 + lane / LANES, next);                           // (nobody's rows lie in the tensors too)
+    kv8_check_batch(P, unit, P.n_rows * io.groups, lane);
     Kv8Seq s;
     if (!kv8_seq_of_row(P, r, lane, &s)) return;
     const int64_t at = kv8_place(P, s, r);
@@ -165,6 +166,7 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Io io) {
     const int r = unit / io.groups;
     if (r >= P.n_rows) return;
     const int h0 = (int)(unit - (uint32_t)r * io.groups) * io.heads, h1 = min(h0 + io.heads, P.hkv);
+    kv8_check_batch(P, unit, P.n_rows * io.groups, lane);
     Kv8Seq s;
     if (!kv8_seq_of_row(P, r, lane, &s)) return;
     const int64_t at = kv8_place(P, s, r);
@@ -249,6 +251,7 @@ constexpr int kRowsStages = 3;
 constexpr int kRowsWarps = 4;
 constexpr float kLazy = 2.f;
 constexpr float kWeightUnit = 2048.f;
+constexpr float kPartShare = 0x1p-8f;                            // parts (256 at most) join with weights up to this: large results do not overflow
 
 __device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
     uint32_t r;
@@ -586,11 +589,13 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_ker
                 sum += __shfl_xor_sync(~0u, sum, 4);
                 sum += __shfl_xor_sync(~0u, sum, 8);
                 sum += __shfl_xor_sync(~0u, sum, 16);
+                // (divided by the warp's own sum first: a sum over many tokens of large numbers is beyond fp32)
+                const float inv = sum > 0.f ? 1.f / sum : sum;
                 float *a = acc + (warp * R + row) * D + gi * (D / 8);
 #pragma unroll
                 for (int x = 0; x < D / 16; ++x) {
-                    a[2 * x] = o[nb][x][y] * unit;
-                    a[2 * x + 1] = o[nb][x][y + 2] * unit;
+                    a[2 * x] = o[nb][x][y] * inv * unit;
+                    a[2 * x + 1] = o[nb][x][y + 2] * inv * unit;
                 }
                 // (a row whose every score is NaN has no maximum, and is not an empty row)
                 if (gi == 0) { ml[(warp * R + row) * 2] = sum != sum ? sum : -nm[nb][y]; ml[(warp * R + row) * 2 + 1] = sum; }
@@ -605,16 +610,20 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_ker
                 const float mw = ml[(w * R + row) * 2];
                 top = (mw > top || mw != mw) ? mw : top;
             }
-            float sum = 0.f, a0 = 0.f, a1 = 0.f;
+            float f[kRowsWarps], sum = 0.f, a0 = 0.f, a1 = 0.f;
 #pragma unroll
             for (int w = 0; w < kRowsWarps; ++w) {
-                const float mw = ml[(w * R + row) * 2], f = mw == -INFINITY ? 0.f : ex2_approx(mw - top);
-                sum += f * ml[(w * R + row) * 2 + 1];
-                a0 += f * acc[(w * R + row) * D + ch];
-                a1 += f * acc[(w * R + row) * D + ch + 1];
+                const float mw = ml[(w * R + row) * 2];
+                f[w] = mw == -INFINITY ? 0.f : ex2_approx(mw - top) * ml[(w * R + row) * 2 + 1];
+                sum += f[w];
             }
             const bool empty = top == -INFINITY;
-            if (empty) { a0 = a1 = 0.f; } else { a0 /= sum; a1 /= sum; }
+            const float inv = empty ? 0.f : 1.f / sum;
+#pragma unroll
+            for (int w = 0; w < kRowsWarps; ++w) {
+                a0 += f[w] * inv * acc[(w * R + row) * D + ch];
+                a1 += f[w] * inv * acc[(w * R + row) * D + ch + 1];
+            }
             const int tok = (pair0 + row) / A.group, head = kvh * A.group + (pair0 + row) % A.group;
             const float lse2 = empty ? -INFINITY : top + log2f(sum);
             if (parts == 1) {
@@ -645,7 +654,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_ker
                     nan |= y != y;
                 }
                 for (int p = 0; p < parts; ++p) {
-                    const float y = cluster_load(at_lse + row * 4, p), f = y == -INFINITY ? 0.f : ex2_approx(y - top);
+                    const float y = cluster_load(at_lse + row * 4, p), f = y == -INFINITY ? 0.f : kPartShare * ex2_approx(y - top);
                     const float2 v = cluster_load2(at + (row * D + ch) * 4, p);
                     sum += f;
                     a0 += f * v.x;
@@ -656,7 +665,7 @@ __global__ void __launch_bounds__(kRowsWarps * 32, NB == 1 ? 4 : 2) kv8_rows_ker
                 *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(A.out) + (int64_t)(s.start + tok) * A.o_rs +
                                               (int64_t)head * A.o_hs + ch) = empty ? 0u : float2_to_pair(a0 / sum, a1 / sum, A.bf16);
                 if (A.lse && ch == 0)
-                    A.lse[(int64_t)(s.start + tok) * A.hq + head] = empty ? -INFINITY : (top + log2f(sum)) * kLn2;
+                    A.lse[(int64_t)(s.start + tok) * A.hq + head] = empty ? -INFINITY : (top + log2f(sum * (1.f / kPartShare))) * kLn2;
             }
             cluster_sync();                                      // nobody's results are overwritten or gone while another reads them
         }
@@ -705,7 +714,7 @@ __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Params P, const 
         for (int x = 0; x < D / 32; ++x) a[x] = 0.f;
 #pragma unroll 4
         for (int i = WIDE ? warp : 0; i < parts; i += WIDE ? 4 : 1) {
-            const float f = pl[i] == -INFINITY ? 0.f : ex2_approx(pl[i] - top);
+            const float f = pl[i] == -INFINITY ? 0.f : kPartShare * ex2_approx(pl[i] - top);
             sum += f;
 #pragma unroll
             for (int x = 0; x < D / 64; ++x) {
@@ -735,7 +744,7 @@ __global__ void __launch_bounds__(128) kv8_join_kernel(const Kv8Params P, const 
             *reinterpret_cast<uint32_t *>(op + x * 64 + lane * 2) =
                 empty ? 0u : float2_to_pair(a[2 * x] / sum, a[2 * x + 1] / sum, A.bf16);
         if (A.lse && lane == 0)
-            A.lse[(int64_t)(s.start + tok) * A.hq + head] = empty ? -INFINITY : (top + log2f(sum)) * kLn2;
+            A.lse[(int64_t)(s.start + tok) * A.hq + head] = empty ? -INFINITY : (top + log2f(sum * (1.f / kPartShare))) * kLn2;
     }
 }
 

@@ -76,6 +76,13 @@ __device__ __forceinline__ Kv8Seq kv8_seq_from_lane(const Kv8Seq &s, int b, int 
     return {b, __shfl_sync(~0u, s.start, src), __shfl_sync(~0u, s.n, src), __shfl_sync(~0u, s.kv, src)};
 }
 
+// Whole warp `first` of `step`: a share of the sequences is looked at for what does not fit. (Up to 32 are looked at by every
+// warp that walks over them; of more, those without rows might be passed over by all.)
+__device__ __forceinline__ void kv8_check_batch(const Kv8Params &P, uint32_t first, uint32_t step, int lane) {
+    if (P.n_seqs <= 32 || !P.status) return;
+    for (uint64_t i = first; i * 32 < (uint32_t)P.n_seqs; i += step) (void)kv8_seq(P, (int)i * 32 + lane);
+}
+
 // Whole warp: the sequence that row r belongs to; false if it is nobody's. row_start is searched 32 entries at a time.
 __device__ __forceinline__ bool kv8_seq_of_row(const Kv8Params &P, int r, int lane, Kv8Seq *out) {
     int base = 0, count = P.n_seqs;

@@ -186,6 +186,8 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
             }
         }
         if (lane == 0) work_s.go = go;
+    } else if (warp == 1 && blockIdx.z == 0) {
+        kv8_check_batch(P, blockIdx.x, gridDim.x, lane);
     }
     __syncthreads();
     if (!W.go) return;
@@ -425,8 +427,9 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
             if (!failed && n_tiles > 0 && !warp_wait(bar(kBarO + qt), 0)) failed = true;
             tc_fence_after_sync();
             if (!failed) {
-                float sigma = 0.f;
-                if (n_tiles > 0) sigma = reinterpret_cast<const float *>(smem + M::kScales + ((n_tiles - 1) & 3) * M::kStage + M::kFirst)[5];
+                float unit = 0.f;                                // sigma / kTlWeightUnit; a factor of its own: with 1 / l it may be subnormal
+                if (n_tiles > 0)
+                    unit = reinterpret_cast<const float *>(smem + M::kScales + ((n_tiles - 1) & 3) * M::kStage + M::kFirst)[5] * (1.f / kTlWeightUnit);
                 const int parts = W.parts;
                 float inv[2];
                 bool live[2];
@@ -439,7 +442,7 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
                     l += __shfl_xor_sync(~0u, l, 1);
                     l += __shfl_xor_sync(~0u, l, 2);
                     const bool empty = l == 0.f;
-                    inv[q] = empty ? 0.f : 1.f / l * (1.f / kTlWeightUnit) * sigma;
+                    inv[q] = empty ? 0.f : 1.f / l;
                     const float lse2 = empty ? -INFINITY : log2f(l) - unpack2(nm2[q]).x;
                     const int r = qt * kTlRows + row0 + 8 * q + gi, pair = W.pair0 + r, tok = W.start + pair / A.group;
                     const int head = (int)(blockIdx.x % P.hkv) * A.group + pair % A.group;
@@ -465,8 +468,8 @@ __global__ void __launch_bounds__(kTlThreads, 1) kv8_tiles_kernel(const Kv8Param
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
                             if (!live[q]) continue;
-                            const float u = n_tiles > 0 ? __uint_as_float(ov[b * 4 + q * 2]) * inv[q] : 0.f;
-                            const float v = n_tiles > 0 ? __uint_as_float(ov[b * 4 + q * 2 + 1]) * inv[q] : 0.f;
+                            const float u = n_tiles > 0 ? __uint_as_float(ov[b * 4 + q * 2]) * inv[q] * unit : 0.f;
+                            const float v = n_tiles > 0 ? __uint_as_float(ov[b * 4 + q * 2 + 1]) * inv[q] * unit : 0.f;
                             if (parts == 1) *reinterpret_cast<uint32_t *>(op[q] + c + b * 8) = float2_to_pair(u, v, A.bf16);
                             else *reinterpret_cast<float2 *>(pa[q] + c + b * 8) = make_float2(u, v);
                         }

@@ -525,3 +525,60 @@ def test_queries_of_any_size(binding):
         q[1] = 0
         got, lse = pages.h1b_kv8_attention(q.cuda(), *b.tensors(), scale=0.1 / size, return_lse=True)
         check_attention(got, lse, attention(q, pool, b, "int8", 0.1 / size))
+
+
+@pytest.mark.parametrize("n,kv", [(1, 5000), (2, 300), (140, 2000), (60, 700)])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_powers_of_two_pass_through(binding, n, kv, fmt):
+    """Values times a power of two are results times that power, to the bit, and keys against queries likewise: up to sums over
+    the tokens that fp32 cannot hold (all values positive and alike: 2^125 and their sum 2^137), and down to 2^-100."""
+    b, hq, hkv, d = Batch([n, n], [kv, kv - 7], 64, seed=2), 8, 2, 128
+    k, v, ks, vs = filled_pool(b, hkv, d, fmt, 2, BF16)
+    v = v.view(torch.uint8).bitwise_and(0x7F).clamp(max=0x7E).view(v.dtype)
+    vs = torch.where(vs.isnan(), vs, torch.exp2(torch.floor(torch.log2(vs))))
+    g = torch.Generator().manual_seed(4)
+    q = torch.randn(b.n_rows, hq, d, generator=g).to(BF16)
+
+    def run(q_pow, k_pow, v_pow, scale=0.02):
+        pages = pages_of(binding, (k, v, ks * 2.0 ** k_pow, vs * 2.0 ** v_pow))
+        out, lse = pages.h1b_kv8_attention((q.double() * 2.0 ** q_pow).to(BF16).cuda(), *b.tensors(), scale=scale, max_rows=n,
+                                           return_lse=True)
+        pages.h1b_kv8_poll_status()
+        return out.double().cpu(), lse.cpu()
+
+    top = 125 - int(torch.log2(vs[~vs.isnan()].max() * {"int8": 127, "e4m3": 448}[fmt]).floor())
+    for scale in (0.02, 0.0):
+        want, want_lse = run(0, 0, 0, scale)
+        assert want.isfinite().all() and (want > 0).all()
+        for powers in ((0, 0, top), (0, 0, -100), (-80, 80, 0), (20, -20, 3)):
+            got, lse = run(*powers, scale)
+            assert torch.equal(got, want * 2.0 ** powers[2]), powers
+            assert torch.equal(lse, want_lse), powers
+
+
+@pytest.mark.parametrize("n", [1, 33])
+@pytest.mark.parametrize("what", ["row_start", "kv_len", "capacity"])
+def test_sequences_without_rows_are_checked_too(binding, n, what):
+    """Of many sequences, one that has no rows does not fit: each call says so, and computes the others."""
+    seqs, hq, hkv, d = 120, 2, 1, 64
+    rows = [n if s % 40 == 7 else 0 for s in range(seqs)]
+    b = Batch(rows, [40] * seqs, 16, seed=1)
+    table, kv_len, row_start = b.tensors()
+    if what == "row_start":
+        row_start[100] = 10 ** 6                           # (behind the last row: up and down again)
+    elif what == "kv_len":
+        kv_len[70] = -1
+    else:
+        kv_len[119] = 49
+    pages = pages_of(binding, filled_pool(b, hkv, d, "int8", 1))
+    x = torch.randn(b.n_rows, hkv, d, generator=torch.Generator().manual_seed(1)).half().cuda()
+    q = torch.randn(b.n_rows, hq, d, generator=torch.Generator().manual_seed(2)).half().cuda()
+    calls = [lambda: pages.h1b_kv8_append(x, x, table, kv_len, row_start),
+             lambda: pages.h1b_kv8_read(table, kv_len, row_start, n_rows=b.n_rows),
+             lambda: pages.h1b_kv8_attention(q, table, kv_len, row_start, scale=1.0, max_rows=n),
+             lambda: pages.h1b_kv8_attention(q, table, kv_len, row_start, scale=1.0, max_rows=64)]
+    for call in calls:
+        call()
+        with pytest.raises(binding.H1BError):
+            pages.h1b_kv8_poll_status()
+        pages.h1b_kv8_poll_status()                        # (once)
