@@ -9,10 +9,13 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------------------------
 // Append and read. A row of d numbers is handled by d / 16 lanes (8 numbers of each half of the row, so that neighbouring
-// lanes read and write neighbouring bytes), the keys and values of two
-// (d = 128) or four heads side by side in one warp; a warp takes `heads` KV heads of one row, so the walk over the batch and
-// the page table is done once for all of them, and the next heads' loads are under way while it works on these. Both are
-// bound by memory: a token of a head is 2 * 2 d bytes on one side and 2 (d + 4) on the other.
+// lanes read and write neighbouring bytes), the keys and values of two (d = 128) or four heads side by side in one warp; a
+// warp takes `heads` KV heads of one row, so the walk over the batch and the page table is done once for all of them, and the
+// next heads' loads are under way while it works on these. A token of a head is 2 * 2 d bytes on one side and 2 (d + 4) on
+// the other. Read is bound by memory: 8 sequences of 2-4k tokens, 32 heads of 128, 99 us = 6.1 TB/s, 94 % of the copy
+// bandwidth. Append is bound by instruction issue (75 % of the slots; some 18 instructions a number): 8192 tokens of 32 heads
+// of 128, 45.6 us = 4.5 TB/s, 68 %; with a division for each number it was 82. A grid of as many blocks as run at once, each
+// looping over rows, took 47.6 and (read) 130 us.
 // ------------------------------------------------------------------------------------------------------------------
 struct Kv8Io {
     Kv8Params P;
@@ -246,6 +249,9 @@ cudaError_t launch_io(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_r
 // carried times 2^11, stay below 2^15 and keep fp16's full precision down to 2^-25 of the largest one. One rounding to fp16
 // (2^-12 on average) vanishes beside that of a bf16 result, but would add as much again to an fp16 result's: there (SPLIT)
 // a second product carries what the rounding left, w = hi + lo to 2^-22, at no cost in time where the loads are the bound.
+// Bound by memory where there is enough of it: 16 sequences of 4-8k tokens, 32 heads of 128 (int8, fp16): 150 us = 5.7 TB/s,
+// 87 % of the copy bandwidth, the arithmetic pipe that unpacks codes busy 53 % of the time; 8 of 32k, 32 / 8 heads (e4m3,
+// bf16): 97 us, 86 %. tcgen05 has no place here: its smallest tile is 64 rows, and codes would pass shared memory twice.
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int kRowsStages = 3;
 constexpr int kRowsWarps = 4;
