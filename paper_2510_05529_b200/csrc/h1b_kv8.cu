@@ -13,9 +13,9 @@ namespace {
 // warp takes `heads` KV heads of one row, so the walk over the batch and the page table is done once for all of them, and the
 // next heads' loads are under way while it works on these. A token of a head is 2 * 2 d bytes on one side and 2 (d + 4) on
 // the other. Read is bound by memory: 8 sequences of 2-4k tokens, 32 heads of 128, 99 us = 6.1 TB/s, 94 % of the copy
-// bandwidth. Append is bound by instruction issue (75 % of the slots; some 18 instructions a number): 8192 tokens of 32 heads
-// of 128, 45.6 us = 4.5 TB/s, 68 %; with a division for each number it was 82. A grid of as many blocks as run at once, each
-// looping over rows, took 47.6 and (read) 130 us.
+// bandwidth. Append is bound by instruction issue (75 % of the slots; some 14 instructions a number): 8192 tokens of 32 heads
+// of 128, 41.6 us = 4.9 TB/s, 74 %; with a division for each number it was 82, with a lane's addresses computed for each head
+// 44.7. A grid of as many blocks as run at once, each looping over rows, took longer (append 2 us, read 30).
 // ------------------------------------------------------------------------------------------------------------------
 struct Kv8Io {
     Kv8Params P;
@@ -98,6 +98,16 @@ __device__ __forceinline__ uint4 kv8_quantise16(const float (&f)[16], float amax
     return make_uint4(c[0], c[1], c[2], c[3]);
 }
 
+// amax / TOP, rounded once. The product with 1 / TOP, corrected by its remainder, is the correctly rounded quotient (P. Markstein,
+// IA-64 and Elementary Functions, 2000; all 1024 mantissas that an amax may have were compared); not where a term is subnormal.
+template <int FMT>
+__device__ __forceinline__ float kv8_scale(float amax) {
+    constexpr float TOP = FMT == H1B_KV8_INT8 ? 127.f : 448.f, BY = 1.f / TOP;
+    if (amax < 0x1p-80f) return __fdiv_rn(amax, TOP);
+    const float q = amax * BY;
+    return fmaf(fmaf(-q, TOP, amax), BY, q);
+}
+
 // The largest magnitude; NaN if there is one.
 __device__ __forceinline__ float max_abs(float a, float b, float c) {
     float r;
@@ -108,35 +118,39 @@ __device__ __forceinline__ float max_abs(float a, float b, float c) {
 template <int D, int FMT, bool BF16>
 __global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Io io) {
     constexpr int LANES = D / 16, VECS = 32 / LANES;             // lanes per vector, vectors (key or value rows) per warp
-    constexpr float TOP = FMT == H1B_KV8_INT8 ? 127.f : 448.f;
     const Kv8Params &P = io.P;
     const int lane = threadIdx.x & 31, sub = lane % LANES;
     const uint32_t unit = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
     const int r = unit / io.groups;
     if (r >= P.n_rows) return;                                   // (whole warps)
     const int h0 = (int)(unit - (uint32_t)r * io.groups) * io.heads, h1 = min(h0 + io.heads, P.hkv);
-    // vector x of the row: head x / 2, its key (x even) or value
-    const uint16_t *src_k = static_cast<const uint16_t *>(io.k.data) + (int64_t)r * io.k.row_stride + sub * 8;
-    const uint16_t *src_v = static_cast<const uint16_t *>(io.v.data) + (int64_t)r * io.v.row_stride + sub * 8;
-    auto load = [&](int x, uint4 (&w)[2]) {
-        w[0] = w[1] = make_uint4(0, 0, 0, 0);
-        if ((x >> 1) >= h1) return;
-        const uint16_t *p = (x & 1) ? src_v + (int64_t)(x >> 1) * io.v.head_stride : src_k + (int64_t)(x >> 1) * io.k.head_stride;
-        w[0] = __ldcs(reinterpret_cast<const uint4 *>(p));
-        w[1] = __ldcs(reinterpret_cast<const uint4 *>(p + D / 2));
+    // A lane has the keys (val: the values) of head h, then of the head HEADS further on ...
+    constexpr int HEADS = VECS / 2;
+    const bool val = (lane / LANES) & 1;
+    int h = h0 + lane / (2 * LANES);
+    const int64_t hop = (val ? io.v.head_stride : io.k.head_stride) * HEADS;
+    const uint16_t *src = static_cast<const uint16_t *>(val ? io.v.data : io.k.data) +
+                          (int64_t)r * (val ? io.v.row_stride : io.k.row_stride) +
+                          (int64_t)h * (val ? io.v.head_stride : io.k.head_stride) + sub * 8;
+    auto load = [&](uint4 (&w)[2]) {
+        w[0] = __ldcs(reinterpret_cast<const uint4 *>(src));
+        w[1] = __ldcs(reinterpret_cast<const uint4 *>(src + D / 2));
     };
-    uint4 next[2];
-    load(h0 * 2 + lane / LANES, next);                           // (nobody's rows lie in the tensors too)
+    uint4 next[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+    if (h < h1) load(next);                                      // (nobody's rows lie in the tensors too)
     kv8_check_batch(P, unit, P.n_rows * io.groups, lane);
     Kv8Seq s;
     if (!kv8_seq_of_row(P, r, lane, &s)) return;
     const int64_t at = kv8_place(P, s, r);
     if (at < 0) return;
+    const int64_t row = at + (int64_t)h * P.page_tokens, next_row = (int64_t)HEADS * P.page_tokens;
+    uint8_t *to = (val ? P.v : P.k) + row * D + sub * 8;
+    float *scale = (val ? P.vs : P.ks) + row;
 #pragma unroll 1
-    for (int x0 = h0 * 2; x0 < h1 * 2; x0 += VECS) {
-        const int x = x0 + lane / LANES, h = x >> 1;
+    for (int hb = h0; hb < h1; hb += HEADS, h += HEADS, to += next_row * D, scale += next_row) {
         const uint32_t w[8] = {next[0].x, next[0].y, next[0].z, next[0].w, next[1].x, next[1].y, next[1].z, next[1].w};
-        if (x0 + VECS < h1 * 2) load(x + VECS, next);
+        src += hop;
+        if (h + HEADS < h1) load(next);
         float f[16], amax = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -150,11 +164,9 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Io io) {
         uint4 c = make_uint4(0, 0, 0, 0);
         if (!odd && amax > 0.f) c = kv8_quantise16<FMT>(f, amax);
         if (h < h1) {
-            const int64_t row = at + (int64_t)h * P.page_tokens;
-            uint8_t *to = ((x & 1) ? P.v : P.k) + row * D + sub * 8;
             *reinterpret_cast<uint2 *>(to) = make_uint2(c.x, c.y);
             *reinterpret_cast<uint2 *>(to + D / 2) = make_uint2(c.z, c.w);
-            if (sub == 0) ((x & 1) ? P.vs : P.ks)[row] = odd ? __int_as_float(0x7FC00000) : __fdiv_rn(amax, TOP);
+            if (sub == 0) *scale = odd ? __int_as_float(0x7FC00000) : kv8_scale<FMT>(amax);
         }
         __syncwarp();
     }
@@ -225,7 +237,8 @@ cudaError_t launch_io(const Kv8Params &P, const h1b_kv8_rows &k, const h1b_kv8_r
     while (io.heads < 16 && (int64_t)P.n_rows * ((P.hkv + io.heads - 1) / io.heads) > 148 * 64) io.heads *= 2;
     io.groups = (P.hkv + io.heads - 1) / io.heads;
     const int64_t warps = (int64_t)P.n_rows * io.groups;
-    const int warps_per_block = warps < 148 * 8 ? 1 : 8;
+    // (smaller blocks even append's warps out, some of which divide: 8192 tokens 41.6 us, 42.4 with eight warps; read 100 and 99)
+    const int warps_per_block = warps < 148 * 8 ? 1 : APPEND ? 4 : 8;
     const unsigned grid = (unsigned)((warps + warps_per_block - 1) / warps_per_block);
 #define H1B_KV8_IO(D, F, B)                                                                                            \
     kv8_launch(APPEND ? kv8_append_kernel<D, F, B> : kv8_read_kernel<D, F, B>, dim3(grid), warps_per_block * 32, 0, st, io)

@@ -582,3 +582,32 @@ def test_sequences_without_rows_are_checked_too(binding, n, what):
         with pytest.raises(binding.H1BError):
             pages.h1b_kv8_poll_status()
         pages.h1b_kv8_poll_status()                        # (once)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+def test_many_rows_are_appended_and_read_like_few(binding, d, fmt):
+    """A warp takes more heads where there are many rows: the same bits as row for row in small calls."""
+    rows, hkv, page = [3000, 0, 2300], 21, 32
+    b = Batch(rows, [3000, 9, 2404], page, seed=6)
+    g = torch.Generator().manual_seed(3)
+    k, v = (torch.randn(b.n_rows, hkv, d, generator=g).to(BF16).cuda() for _ in "kv")
+    table, kv_len, row_start = b.tensors()
+    one, many = (pages_of(binding, empty_pool(b.n_pages, hkv, page, d, fmt)) for _ in "ab")
+    one.h1b_kv8_append(k, v, table, kv_len, row_start)
+    wk, wv = one.h1b_kv8_read(table, kv_len, row_start, n_rows=b.n_rows, dtype=BF16)
+    step, r = 100, 0
+    for s in (0, 2):
+        for at in range(0, rows[s], step):
+            part = (table[s:s + 1], torch.tensor([b.kv[s] - rows[s] + at + step], dtype=torch.int32, device="cuda"),
+                    torch.tensor([0, step], dtype=torch.int32, device="cuda"))
+            many.h1b_kv8_append(k[r:r + step], v[r:r + step], *part)
+            gk, gv = one.h1b_kv8_read(*part, n_rows=step, dtype=BF16)
+            assert torch.equal(gk, wk[r:r + step]) and torch.equal(gv, wv[r:r + step])
+            r += step
+    for p in (one, many):
+        p.h1b_kv8_poll_status()
+    for a, c in zip((one.k_pages, one.v_pages, one.k_scale, one.v_scale), (many.k_pages, many.v_pages, many.k_scale, many.v_scale)):
+        assert torch.equal(a.view(torch.uint8), c.view(torch.uint8))
+    # half a step of the codes at amax, and the rounding to bf16
+    assert (wk.double() - k.double()).abs().max() <= ({"int8": 0.5 / 127, "e4m3": 16 / 448}[fmt] + 2.0 ** -8) * k.double().abs().max()
