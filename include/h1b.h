@@ -537,6 +537,8 @@ int h1b_kv8_read(const h1b_kv8_pool *pool, const h1b_kv8_batch *batch, const h1b
  *   q, out  [n_rows][Hq][d] of type `dtype`; out = softmax(scale q k) v. Sums,
  *           maxima and products are held in fp32; the weights are rounded to
  *           fp16 before they multiply the values.
+ *           out may be q itself (same data and strides), and must not overlap it
+ *           otherwise.
  *   lse     DEVICE fp32 [n_rows][Hq], nullable: the natural logarithm of the
  *           sum of exp(scale q k) over the tokens seen (for joining the result
  *           with attention over other tokens). A row that sees nothing gets

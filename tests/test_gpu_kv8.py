@@ -611,3 +611,15 @@ def test_many_rows_are_appended_and_read_like_few(binding, d, fmt):
         assert torch.equal(a.view(torch.uint8), c.view(torch.uint8))
     # half a step of the codes at amax, and the rounding to bf16
     assert (wk.double() - k.double()).abs().max() <= ({"int8": 0.5 / 127, "e4m3": 16 / 448}[fmt] + 2.0 ** -8) * k.double().abs().max()
+
+
+@pytest.mark.parametrize("rows,kv", [([1], [700]), ([1] * 3, [40, 9000, 5000]), ([1], [20000]), ([150, 1, 40], [6000, 5000, 900]), ([300], [300])])
+def test_the_result_may_take_the_place_of_q(binding, rows, kv):
+    hq, hkv, d = 8, 2, 128
+    b = Batch(rows, kv, 64, seed=4)
+    pages = pages_of(binding, filled_pool(b, hkv, d, "int8", 4, BF16))
+    q = torch.randn(b.n_rows, hq, d, generator=torch.Generator().manual_seed(1)).to(BF16).cuda()
+    want = pages.h1b_kv8_attention(q, *b.tensors(), scale=0.1, max_rows=max(rows))
+    assert pages.h1b_kv8_attention(q, *b.tensors(), scale=0.1, max_rows=max(rows), out=q) is q
+    pages.h1b_kv8_poll_status()
+    assert torch.equal(q, want)
